@@ -481,6 +481,95 @@ int slim_linear_gemm_fp8(const slim_layer *layer, const uint8_t *X8, const float
                          slim_half *Y, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * 8-bit layers with a scale for each block of 128: for layers that are not
+ * compressed to 4 bits (a model's most sensitive projections, its scores of the
+ * vocabulary), weights and inputs in E4M3 (App. "Input Quantization" quantizes
+ * inputs to this format with one scale per tensor; here a scale covers 128 inputs
+ * of a token, or 128 x 128 weights).  Of a block z, all in binary32:
+ *   top   = max(max |z|, 2^-100),   scale = top / 448,
+ *   code  = E4M3(z * (448 / top)),  nearest, ties to even, subnormals kept;
+ *   value = code * scale.
+ * A block that holds a NaN has a NaN for its scale and NaN codes; one that holds an infinity has an
+ * infinite scale (infinite values become NaN codes, finite ones zeros).  k need not be a multiple of 128: a row of
+ * codes is kb = ceil(k / 128) whole blocks, zero codes from input k on.
+ *   inputs   codes [m][128 kb] row-major, scales fp32 [m][kb]      (slim_block_fp8_sizes);
+ *   weights  codes in tiles of 64 rows x 128 inputs (8 KiB), row tile major, kb tiles
+ *            per row tile, rows padded to 64 with zero codes; inside a tile the byte
+ *            of row 16 g + 4 t + r, input 64 h + 16 q + b is at
+ *            2048 t + 1024 h + 256 q + 64 g + 16 r + b;  scales fp32
+ *            [ceil(n / 128)][kb]                                   (slim_block_fp8_weight_sizes).
+ * The tile is the order in which the matrix instructions hold their operand.
+ * Matrices in 16 and 32 bits (X, residual, gain, H, Y, G, U, W) may have any alignment of
+ * whole elements and a row stride (`_ld`, in elements, at least the row's length);
+ * codes and workspaces are 16-byte aligned, scales to 4, and without gaps (any run of whole
+ * tokens of an input is an input).  k <= 2^22.
+ */
+typedef enum { SLIM_F16 = 0, SLIM_BF16 = 1, SLIM_F32 = 2 } slim_dtype;
+typedef enum { SLIM_ACT_NONE = 0, SLIM_ACT_SILU = 1 } slim_act;
+
+/* Sizes in bytes (HOST out-pointers, NULL individually).  Errors: SHAPE (m, n, k < 1, k > 2^22). */
+int slim_block_fp8_sizes(int32_t m, int32_t k, size_t *codes_bytes, size_t *scales_bytes);
+int slim_block_fp8_weight_sizes(int32_t n, int32_t k, size_t *codes_bytes, size_t *scales_bytes);
+
+/*
+ * slim_block_fp8_norm -- the residual's addition, the root-mean-square norm and the
+ * quantization of its output, one pass over the row:
+ *   h = X + residual;   y = h * gain / sqrt(mean(h^2) + eps);   codes, scales of y,
+ * h and the sum in binary32.  H and Y, where they are given, receive h and y rounded once
+ * to the row's type.  The codes are those of h * gain, which has the same ones: the row's
+ * factor is in the scales alone.  (So a row whose squares overflow has scales and y of zero, as 1 / sqrt(inf) is.)
+ *   X, residual [m][k] of `dtype` (SLIM_F16, SLIM_BF16); residual may be NULL (h = X);
+ *   gain [k] of `dtype` or SLIM_F32 (`gain_dtype`), NULL: 1;
+ *   H, Y [m][k] out, may be NULL; either may be X or residual itself (same pointer and stride).
+ * Errors: NULL, SHAPE (also a type, a stride, eps negative or NaN), ALIGN, HIP.
+ */
+int slim_block_fp8_norm(const void *X, int64_t x_ld, const void *residual, int64_t residual_ld, const void *gain,
+                        int32_t gain_dtype, int32_t dtype, int32_t m, int32_t k, float eps, void *H, int64_t h_ld,
+                        void *Y, int64_t y_ld, uint8_t *codes, float *scales, void *stream);
+
+/*
+ * slim_block_fp8_act -- codes and scales of act(G) * U, [m][k] of SLIM_F16 or SLIM_BF16:
+ * act SLIM_ACT_SILU (g / (1 + exp(-g))) or SLIM_ACT_NONE; U may be NULL (act(G) alone; with
+ * SLIM_ACT_NONE the plain quantization of an input).  G and U may be the halves of one matrix (strides).
+ * Errors: NULL, SHAPE, ALIGN, HIP.
+ */
+int slim_block_fp8_act(const void *G, int64_t g_ld, const void *U, int64_t u_ld, int32_t act, int32_t dtype, int32_t m,
+                       int32_t k, uint8_t *codes, float *scales, void *stream);
+
+/*
+ * slim_block_fp8_weight -- W [n][k] of any slim_dtype to 8-bit weights: codes in tiles and scales.
+ * slim_block_fp8_tile -- row-major codes [n][k] (row stride ld bytes, any alignment) to tiles, for weights that are in 8 bits
+ * already; slim_block_fp8_untile is its inverse.  No arithmetic.
+ * Errors: NULL, SHAPE, ALIGN, HIP.
+ */
+int slim_block_fp8_weight(const void *W, int64_t ld, int32_t dtype, int32_t n, int32_t k, uint8_t *codes, float *scales,
+                          void *stream);
+int slim_block_fp8_tile(const uint8_t *in, int64_t ld, int32_t n, int32_t k, uint8_t *codes, void *stream);
+int slim_block_fp8_untile(const uint8_t *codes, int32_t n, int32_t k, uint8_t *out, int64_t ld, void *stream);
+
+/* One layer of 8-bit weights: device pointers to caller-owned buffers. */
+typedef struct {
+    int32_t n, k;
+    const uint8_t *codes;   /* in tiles                        */
+    const float *scales;    /* [ceil(n / 128)][ceil(k / 128)]  */
+} slim_block_fp8_layer;
+
+/*
+ * slim_block_fp8_gemm -- Y = X W^T on 8-bit inputs and weights, any m >= 1:
+ *   Y[t][o] = sum_b x_scales[t][b] scales[o / 128][b] sum_{i in block b} X[t][i] W[o][i],
+ * sums in binary32, Y [m][n] rounded once to `dtype` (any slim_dtype), row stride y_ld.
+ * The inputs' codes and scales are slim_block_fp8_norm's or slim_block_fp8_act's (or the caller's own, in
+ * their layout).  Results do not depend on the order of workgroups.
+ * workspace: slim_block_fp8_gemm_workspace (HOST out-pointer; the size for m covers every smaller m), ZERO-FILLED
+ * ONCE before its first use; one for calls that follow one another, two for calls that overlap.
+ * Enqueues kernels only and may be captured into a HIP graph.
+ * Errors: NULL, SHAPE, ALIGN, WORKSPACE, HIP.
+ */
+int slim_block_fp8_gemm_workspace(int32_t n, int32_t k, int32_t m, size_t *bytes);
+int slim_block_fp8_gemm(const slim_block_fp8_layer *layer, const uint8_t *X, const float *x_scales, int32_t m, void *Y,
+                        int64_t y_ld, int32_t dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Measurement aids (they compute nothing of the method): what this machine
  * delivers on a plain streaming read and on back-to-back matrix instructions,
  * to set beside the nominal peaks when a kernel's roofline fraction is quoted

@@ -34,6 +34,10 @@ class slim_layer(ctypes.Structure):
                 ("Ls", ctypes.c_void_p), ("Rq", ctypes.c_void_p), ("Rs", ctypes.c_void_p)]
 
 
+class slim_block_fp8_layer(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("k", ctypes.c_int32), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
 SLIM_OK, SLIM_ERR_NULL, SLIM_ERR_SHAPE, SLIM_ERR_ALIGN, SLIM_ERR_WORKSPACE, SLIM_ERR_HIP, SLIM_ERR_WAIT = 0, -1, -2, -3, -4, -5, -6
 
 EXPORTS = ["slim_status_string", "slim_rank_pad", "slim_packed_sizes", "slim_pack", "slim_pack_adapters",
@@ -42,7 +46,9 @@ EXPORTS = ["slim_status_string", "slim_rank_pad", "slim_packed_sizes", "slim_pac
            "slim_adapter_q4_sizes", "slim_pack_adapters_q4", "slim_unpack_adapters_q4", "slim_pack_ex",
            "slim_quant_workspace_bytes", "slim_quant_search", "slim_quant_search_rows", "slim_adapters_workspace_bytes",
            "slim_compute_adapters", "slim_input_quant_fp8", "slim_probe_read", "slim_probe_mfma", "slim_gemm_tile_order", "slim_input_quant_fp8_codes",
-           "slim_linear_gemm_fp8"]
+           "slim_linear_gemm_fp8",
+           "slim_block_fp8_sizes", "slim_block_fp8_weight_sizes", "slim_block_fp8_norm", "slim_block_fp8_act", "slim_block_fp8_weight",
+           "slim_block_fp8_tile", "slim_block_fp8_untile", "slim_block_fp8_gemm_workspace", "slim_block_fp8_gemm"]
 
 
 def lib():
@@ -86,6 +92,16 @@ def lib():
         L.slim_gemm_tile_order.argtypes = [i32, i32, pi32, sz]
         L.slim_input_quant_fp8_codes.argtypes = [vp, sz, vp, vp, vp, vp, sz, vp]
         L.slim_linear_gemm_fp8.argtypes = [ctypes.POINTER(slim_layer), vp, vp, i32, i32, vp, vp, sz, vp]
+        i64, f32 = ctypes.c_int64, ctypes.c_float
+        L.slim_block_fp8_sizes.argtypes = [i32, i32, psz, psz]
+        L.slim_block_fp8_weight_sizes.argtypes = [i32, i32, psz, psz]
+        L.slim_block_fp8_norm.argtypes = [vp, i64, vp, i64, vp, i32, i32, i32, i32, f32, vp, i64, vp, i64, vp, vp, vp]
+        L.slim_block_fp8_act.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, vp]
+        L.slim_block_fp8_weight.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp]
+        L.slim_block_fp8_tile.argtypes = [vp, i64, i32, i32, vp, vp]
+        L.slim_block_fp8_untile.argtypes = [vp, i32, i32, vp, i64, vp]
+        L.slim_block_fp8_gemm_workspace.argtypes = [i32, i32, i32, psz]
+        L.slim_block_fp8_gemm.argtypes = [ctypes.POINTER(slim_block_fp8_layer), vp, vp, i32, vp, i64, i32, vp, sz, vp]
         for name in EXPORTS[2:]:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -557,4 +573,209 @@ def slim_lowrank(X: torch.Tensor, R_pad: torch.Tensor, L_pad: torch.Tensor, n: i
     _check("slim_lowrank", lib().slim_lowrank(_ptr(X), m, _ptr(R_pad), _ptr(L_pad), slim_shape(n, k, rank), rp,
                                               _ptr(Y), 1 if accumulate else 0, _ptr(workspace), workspace.numel(),
                                               _stream(X)))
+    return Y
+
+
+# ---- 8-bit layers with a scale for each block of 128 ----
+DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+ACTS = {"none": 0, "silu": 1}
+_E4M3 = torch.float8_e4m3fn
+
+
+def _matrix(t: torch.Tensor, like: torch.Tensor, name: str, shape=None, dtype=None):
+    """t's row stride; a matrix of whole rows on like's device, whatever lies between them."""
+    if not t.is_cuda or t.device != like.device:
+        raise ValueError(f"{name} must be on the inputs' device")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or t.dtype != (dtype or like.dtype):
+        raise ValueError(f"{name} must be a {dtype or like.dtype} matrix with contiguous rows")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}")
+    ld = t.stride(0)
+    # (the stride of a single row says nothing)
+    return ld if t.shape[0] > 1 else max(ld, t.shape[1])
+
+
+def _code_buffers(m: int, k: int, codes, scales, device):
+    kb = (k + 127) // 128
+    if codes is None:
+        codes = torch.empty(m, kb * 128, dtype=torch.uint8, device=device)
+    elif codes.dtype not in (torch.uint8, _E4M3) or codes.numel() != m * kb * 128 or codes.device != device or not codes.is_contiguous():
+        raise ValueError("codes must be contiguous uint8 [m][128 ceil(k / 128)] on the inputs' device")
+    if scales is None:
+        scales = torch.empty(m, kb, dtype=torch.float32, device=device)
+    elif scales.dtype != torch.float32 or scales.numel() != m * kb or scales.device != device or not scales.is_contiguous():
+        raise ValueError("scales must be contiguous float32 [m][ceil(k / 128)] on the inputs' device")
+    return codes, scales
+
+
+def slim_block_fp8_norm(X: torch.Tensor, gain: torch.Tensor | None = None, eps: float = 1e-5, residual: torch.Tensor | None = None,
+                        codes=None, scales=None, H=None, Y=None):
+    """h = X + residual, y = h gain / sqrt(mean(h^2) + eps) -> (codes uint8 [m][128 kb], scales fp32 [m][kb], H, Y): y in 8 bits with a
+    scale per 128 inputs.  H, Y: True for a new matrix of X's type, or one to write (X or residual itself, for in place);
+    None (returned as such): not wanted.  X, residual, H, Y fp16 or bf16 with any row stride; gain of X's type or fp32."""
+    if X.dtype not in (torch.float16, torch.bfloat16) or X.dim() != 2:
+        raise ValueError("X must be a float16 or bfloat16 matrix")
+    x_ld = _matrix(X, X, "X")
+    m, k = X.shape
+    r_ld = h_ld = y_ld = 0
+    rp = hp = yp = gp = None
+    gt = DTYPES[X.dtype]
+    if residual is not None:
+        r_ld, rp = _matrix(residual, X, "residual", X.shape), residual.data_ptr()
+    if gain is not None:
+        if gain.numel() != k or gain.dtype not in (X.dtype, torch.float32) or gain.device != X.device or not gain.is_contiguous():
+            raise ValueError("gain must be contiguous [k] of X's type or float32 on X's device")
+        gp, gt = gain.data_ptr(), DTYPES[gain.dtype]
+    if H is True:
+        H = torch.empty(m, k, dtype=X.dtype, device=X.device)
+    if Y is True:
+        Y = torch.empty(m, k, dtype=X.dtype, device=X.device)
+    if H is not None:
+        h_ld, hp = _matrix(H, X, "H", X.shape), H.data_ptr()
+    if Y is not None:
+        y_ld, yp = _matrix(Y, X, "Y", X.shape), Y.data_ptr()
+    codes, scales = _code_buffers(m, k, codes, scales, X.device)
+    status = lib().slim_block_fp8_norm(X.data_ptr(), x_ld, rp, r_ld, gp, gt, DTYPES[X.dtype], m, k, eps, hp, h_ld, yp, y_ld, codes.data_ptr(),
+                                       scales.data_ptr(), torch._C._cuda_getCurrentRawStream(X.device.index))
+    if status != SLIM_OK:
+        _check("slim_block_fp8_norm", status)
+    return codes, scales, H, Y
+
+
+def slim_block_fp8_act(G: torch.Tensor, U: torch.Tensor | None = None, act: str = "silu", codes=None, scales=None):
+    """act(G) * U ("silu" or "none"; U None: act(G)) -> (codes uint8 [m][128 kb], scales fp32 [m][kb]).  G, U fp16 or bf16 [m][k] with any
+    row stride: the halves of one product's output, for one.  act="none" without U quantizes an input as it is."""
+    if G.dtype not in (torch.float16, torch.bfloat16) or G.dim() != 2:
+        raise ValueError("G must be a float16 or bfloat16 matrix")
+    if act not in ACTS:
+        raise ValueError("act is 'silu' or 'none'")
+    g_ld = _matrix(G, G, "G")
+    m, k = G.shape
+    u_ld, up = (0, None) if U is None else (_matrix(U, G, "U", G.shape), U.data_ptr())
+    codes, scales = _code_buffers(m, k, codes, scales, G.device)
+    status = lib().slim_block_fp8_act(G.data_ptr(), g_ld, up, u_ld, ACTS[act], DTYPES[G.dtype], m, k, codes.data_ptr(), scales.data_ptr(),
+                                      torch._C._cuda_getCurrentRawStream(G.device.index))
+    if status != SLIM_OK:
+        _check("slim_block_fp8_act", status)
+    return codes, scales
+
+
+def slim_block_fp8_weight_sizes(n: int, k: int) -> dict:
+    c, s = ctypes.c_size_t(), ctypes.c_size_t()
+    _check("slim_block_fp8_weight_sizes", lib().slim_block_fp8_weight_sizes(n, k, c, s))
+    return {"codes": c.value, "scales": s.value}
+
+
+def slim_block_fp8_weight(W: torch.Tensor, codes=None, scales=None):
+    """W [n][k] fp32, fp16 or bf16 (any row stride) -> (codes uint8 in tiles, flat; scales fp32 [ceil(n / 128)][ceil(k / 128)])."""
+    if W.dtype not in DTYPES or W.dim() != 2:
+        raise ValueError("W must be a float32, float16 or bfloat16 matrix")
+    ld = _matrix(W, W, "W")
+    n, k = W.shape
+    size = slim_block_fp8_weight_sizes(n, k)
+    if codes is None:
+        codes = torch.empty(size["codes"], dtype=torch.uint8, device=W.device)
+    if scales is None:
+        scales = torch.empty((n + 127) // 128, (k + 127) // 128, dtype=torch.float32, device=W.device)
+    for t, dt, name in ((codes, torch.uint8, "codes"), (scales, torch.float32, "scales")):
+        if t.dtype != dt or t.numel() * t.element_size() != size[name] or t.device != W.device or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous {dt} of slim_block_fp8_weight_sizes on W's device")
+    _check("slim_block_fp8_weight", lib().slim_block_fp8_weight(_ptr(W), ld, DTYPES[W.dtype], n, k, _ptr(codes), _ptr(scales), _stream(W)))
+    return codes, scales
+
+
+def slim_block_fp8_tile(codes: torch.Tensor) -> torch.Tensor:
+    """Row-major E4M3 codes [n][k] (uint8 or float8_e4m3fn, any row stride) -> uint8 in tiles, flat."""
+    if codes.dtype not in (torch.uint8, _E4M3):
+        raise ValueError("codes must be uint8 or float8_e4m3fn")
+    ld = _matrix(codes, codes, "codes")
+    n, k = codes.shape
+    out = torch.empty(slim_block_fp8_weight_sizes(n, k)["codes"], dtype=torch.uint8, device=codes.device)
+    _check("slim_block_fp8_tile", lib().slim_block_fp8_tile(_ptr(codes), ld, n, k, _ptr(out), _stream(codes)))
+    return out
+
+
+def slim_block_fp8_untile(codes: torch.Tensor, n: int, k: int) -> torch.Tensor:
+    """Inverse of slim_block_fp8_tile: uint8 [n][k]."""
+    _dev(codes, torch.uint8, "codes")
+    if codes.numel() != slim_block_fp8_weight_sizes(n, k)["codes"]:
+        raise ValueError("codes are not an n x k layer's")
+    out = torch.empty(n, k, dtype=torch.uint8, device=codes.device)
+    _check("slim_block_fp8_untile", lib().slim_block_fp8_untile(_ptr(codes), n, k, _ptr(out), k, _stream(codes)))
+    return out
+
+
+@dataclass
+class SlimBlockFp8Weight:
+    """Device buffers of one layer of 8-bit weights (what `slim_block_fp8_layer` points at)."""
+    n: int
+    k: int
+    codes: torch.Tensor            # uint8, in tiles (slim_block_fp8_weight, slim_block_fp8_tile)
+    scales: torch.Tensor           # float32 [ceil(n / 128)][ceil(k / 128)]
+
+    def c_ref(self):
+        """Pointer argument for the product; the buffers are checked when it is made, once per layer and again
+        after any field is assigned."""
+        ref = self.__dict__.get("_ref")
+        if ref is None:
+            size = slim_block_fp8_weight_sizes(self.n, self.k)
+            _dev(self.codes, torch.uint8, "codes")
+            _dev(self.scales, torch.float32, "scales")
+            if self.codes.numel() != size["codes"] or self.scales.numel() * 4 != size["scales"] or self.scales.device != self.codes.device:
+                raise ValueError("codes and scales are not an n x k layer's on one device")
+            cs = slim_block_fp8_layer(self.n, self.k, self.codes.data_ptr(), self.scales.data_ptr())
+            ref = (ctypes.byref(cs), cs)
+            self.__dict__["_ref"] = ref
+        return ref[0]
+
+    def __setattr__(self, name, value):
+        self.__dict__.pop("_ref", None)
+        object.__setattr__(self, name, value)
+
+
+def compress_block_fp8(W: torch.Tensor) -> SlimBlockFp8Weight:
+    """slim_block_fp8_weight into a SlimBlockFp8Weight."""
+    return SlimBlockFp8Weight(W.shape[0], W.shape[1], *slim_block_fp8_weight(W))
+
+
+def slim_block_fp8_gemm_workspace(n: int, k: int, m: int) -> int:
+    out = ctypes.c_size_t()
+    _check("slim_block_fp8_gemm_workspace", lib().slim_block_fp8_gemm_workspace(n, k, m, out))
+    return out.value
+
+
+def alloc_block_fp8_workspace(layer: SlimBlockFp8Weight, m: int) -> torch.Tensor:
+    return torch.zeros(slim_block_fp8_gemm_workspace(layer.n, layer.k, m), dtype=torch.uint8, device=layer.codes.device)
+
+
+def slim_block_fp8_gemm(layer: SlimBlockFp8Weight, codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.float16, Y=None,
+                        workspace=None) -> torch.Tensor:
+    """Y [m][n] = inputs times weights^T on 8-bit inputs as slim_block_fp8_norm and slim_block_fp8_act return them, any m >= 1.
+    Y: a float16, bfloat16 or float32 matrix (any row stride), or None for a new one of `dtype`."""
+    ref = layer.c_ref()
+    kb = (layer.k + 127) // 128
+    if codes.dim() != 2 or codes.shape[1] != kb * 128 or codes.dtype not in (torch.uint8, _E4M3) or not codes.is_contiguous():
+        raise ValueError("codes must be contiguous uint8 [m][128 ceil(k / 128)]")
+    m, device = codes.shape[0], layer.codes.device
+    if scales.dtype != torch.float32 or scales.numel() != m * kb or not scales.is_contiguous():
+        raise ValueError("scales must be contiguous float32 [m][ceil(k / 128)]")
+    if Y is None:
+        if dtype not in DTYPES:
+            raise ValueError("dtype is float16, bfloat16 or float32")
+        Y = torch.empty(m, layer.n, dtype=dtype, device=device)
+        ld = layer.n
+    else:
+        if Y.dtype not in DTYPES:
+            raise ValueError("Y must be float16, bfloat16 or float32")
+        ld = _matrix(Y, Y, "Y", (m, layer.n))
+    if codes.device != device or scales.device != device or Y.device != device:
+        raise ValueError("inputs, Y and the layer must be on one device")
+    if workspace is None:
+        workspace = alloc_block_fp8_workspace(layer, m)
+    elif workspace.device != device:
+        raise ValueError("workspace must be on the layer's device")
+    status = lib().slim_block_fp8_gemm(ref, codes.data_ptr(), scales.data_ptr(), m, Y.data_ptr(), ld, DTYPES[Y.dtype], workspace.data_ptr(),
+                                       workspace.numel(), torch._C._cuda_getCurrentRawStream(device.index))
+    if status != SLIM_OK:
+        _check("slim_block_fp8_gemm", status)
     return Y
