@@ -46,6 +46,12 @@ struct Piece {
     };
     static __device__ __forceinline__ vec load(const typename T::type *p) { return reinterpret_cast<const place *>(p)->v; }
     static __device__ __forceinline__ void store(typename T::type *p, vec v) { reinterpret_cast<place *>(p)->v = v; }
+    // past the caches' turn: for what is not read again soon and would only put out what is
+    static __device__ __forceinline__ void store_streaming(typename T::type *p, vec v)
+    {
+        typedef vec any __attribute__((aligned(sizeof(typename T::type))));
+        __builtin_nontemporal_store(v, reinterpret_cast<any *>(p));
+    }
 };
 
 // N elements of a row from `at` on in 32 bits, zero from element `len` on.

@@ -43,22 +43,22 @@ struct NormArgs {
     bool gain32;
 };
 
-// h of one piece of 8, and z = h gain.
+// h of one piece of 8.
 template <class T>
-__device__ __forceinline__ void norm_load(const NormArgs &a, const typename T::type *x, const typename T::type *res, int at, float (&h)[8])
+__device__ __forceinline__ void norm_load(const NormArgs &a, int64_t row, int at, float (&h)[8])
 {
-    load_piece<T>(x, at, a.k, h);
-    if (res) {
+    typedef typename T::type E;
+    load_piece<T>(static_cast<const E *>(a.X) + row * a.x_ld, at, a.k, h);
+    if (a.res) {
         float r[8];
-        load_piece<T>(res, at, a.k, r);
+        load_piece<T>(static_cast<const E *>(a.res) + row * a.res_ld, at, a.k, r);
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[e] += r[e];
     }
 }
 template <class T>
-__device__ __forceinline__ void norm_gain(const NormArgs &a, int at, const float (&h)[8], float (&z)[8])
+__device__ __forceinline__ void gain_piece(const NormArgs &a, int at, float (&g)[8])
 {
-    float g[8];
     if (!a.gain) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) g[e] = 1.0f;
@@ -67,85 +67,90 @@ __device__ __forceinline__ void norm_gain(const NormArgs &a, int at, const float
     } else {
         load_piece<T>(static_cast<const typename T::type *>(a.gain), at, a.k, g);
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = h[e] * g[e];
 }
 
-// One row per workgroup at a time, NV pieces of 8 values per lane, held in registers from the one read to the last write.
-// LONG: rows that do not fit so are read twice, the sum first.
+// A row per workgroup, NV pieces of 8 values per lane, held in registers from the one read to the last write (more rows than
+// workgroups fit into a grid are walked).  LONG: rows that do not fit so are read twice, the sum first.
+// Bound by memory: 4096 x 8192 in fp16 with a residual moves 236 MB in 48 us, 4.9 TB/s, the rate of a large copy (5.0).  Workgroups that
+// stay and walk the rows with the next row's loads under way, 2 to 32 of them per compute unit, took 48 to 57 us.
 template <class T, int NV, bool LONG>
 __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a)
 {
     typedef typename T::type E;
-    __shared__ float red[16];
+    __shared__ float red[2][16];
     const int kp = a.kb * kBlk, step = 8 * (int)blockDim.x, waves = (int)blockDim.x / kWave, first = 8 * (int)threadIdx.x;
-    for (int64_t row = blockIdx.x; row < a.m; row += gridDim.x) {
-        const E *x = static_cast<const E *>(a.X) + row * a.x_ld;
-        const E *res = a.res ? static_cast<const E *>(a.res) + row * a.res_ld : nullptr;
-        E *H = a.H ? static_cast<E *>(a.H) + row * a.h_ld : nullptr;
-        E *Y = a.Y ? static_cast<E *>(a.Y) + row * a.y_ld : nullptr;
-        uint8_t *codes = a.codes + row * kp;
-        float *scales = a.scales + row * a.kb;
+    int turn = 0;
 
-        auto total = [&](float s) {
-            s = wave_sum(s);
-            if (row != (int64_t)blockIdx.x) __syncthreads();          // the last row's sums have been read
-            if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = s;
+    // 1 / root mean square of a row from this lane's share of its squares' sum
+    auto factor = [&](float s) {
+        s = wave_sum(s);
+        if (waves > 1) {
+            // (two sets in turn: a wavefront that is a row ahead does not overwrite what another still reads)
+            if ((threadIdx.x & (kWave - 1)) == 0) red[turn][threadIdx.x / kWave] = s;
             __syncthreads();
             s = 0.f;
-            for (int w = 0; w < waves; ++w) s += red[w];
-            return 1.0f / sqrtf(s / (float)a.k + a.eps);
-        };
-        // codes of a piece, and what its scale is but for the row's factor (every lane of the block returns it)
-        auto encode = [&](int at, const float(&z)[8]) {
-            const float top = floored_top(block_top(top_of(z)));
-            *reinterpret_cast<uint2_t *>(codes + at) = eight_codes(z, top);
-            return top / kFp8Max;
-        };
-        auto finish = [&](int at, float sc, float rstd, float(&z)[8]) {
-            if ((threadIdx.x & 15) == 0) scales[at / kBlk] = sc * rstd;
-            if (Y) {
+            for (int w = 0; w < waves; ++w) s += red[turn][w];
+            turn ^= 1;
+        }
+        return 1.0f / sqrtf(s / (float)a.k + a.eps);
+    };
+    // codes of a piece, and what its scale is but for the row's factor (every lane of the block returns it)
+    auto encode = [&](int64_t row, int at, const float(&z)[8]) {
+        const float top = floored_top(block_top(top_of(z)));
+        *reinterpret_cast<uint2_t *>(a.codes + row * kp + at) = eight_codes(z, top);
+        return top / kFp8Max;
+    };
+    auto finish = [&](int64_t row, int at, float sc, float rstd, float(&z)[8]) {
+        if ((threadIdx.x & 15) == 0) a.scales[row * a.kb + at / kBlk] = sc * rstd;
+        if (a.Y) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] *= rstd;
-                store_piece<T>(Y, at, a.k, z);
-            }
-        };
+            for (int e = 0; e < 8; ++e) z[e] *= rstd;
+            store_piece<T>(static_cast<E *>(a.Y) + row * a.y_ld, at, a.k, z);
+        }
+    };
 
-        float sum = 0.f;
-        if constexpr (!LONG) {
-            float z[NV][8], sc[NV];
+    if constexpr (!LONG) {
+        for (int64_t row = blockIdx.x; row < a.m; row += gridDim.x) {
+            float z[NV][8], sc[NV], sum = 0.f;
 #pragma unroll
             for (int p = 0; p < NV; ++p)
-                if (first + p * step < kp) norm_load<T>(a, x, res, first + p * step, z[p]);
+                if (first + p * step < kp) norm_load<T>(a, row, first + p * step, z[p]);
 #pragma unroll
             for (int p = 0; p < NV; ++p) {
                 const int at = first + p * step;
                 sc[p] = 0.f;
                 if (at < kp) {
+                    float g[8];
+                    gain_piece<T>(a, at, g);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum += z[p][e] * z[p][e];
-                    if (H) store_piece<T>(H, at, a.k, z[p]);
-                    norm_gain<T>(a, at, z[p], z[p]);
-                    sc[p] = encode(at, z[p]);
+                    if (a.H) store_piece<T>(static_cast<E *>(a.H) + row * a.h_ld, at, a.k, z[p]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[p][e] *= g[e];
+                    sc[p] = encode(row, at, z[p]);
                 }
             }
-            const float rstd = total(sum);
+            const float rstd = factor(sum);
 #pragma unroll
             for (int p = 0; p < NV; ++p)
-                if (first + p * step < kp) finish(first + p * step, sc[p], rstd, z[p]);
-        } else {
-            float h[8];
+                if (first + p * step < kp) finish(row, first + p * step, sc[p], rstd, z[p]);
+        }
+    } else {
+        for (int64_t row = blockIdx.x; row < a.m; row += gridDim.x) {
+            float h[8], g[8], sum = 0.f;
             for (int at = first; at < kp; at += step) {
-                norm_load<T>(a, x, res, at, h);
+                norm_load<T>(a, row, at, h);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum += h[e] * h[e];
             }
-            const float rstd = total(sum);
+            const float rstd = factor(sum);
             for (int at = first; at < kp; at += step) {
-                norm_load<T>(a, x, res, at, h);            // (H or Y may be X or the residual: a piece is read and written by one lane, here last)
-                if (H) store_piece<T>(H, at, a.k, h);
-                norm_gain<T>(a, at, h, h);
-                finish(at, encode(at, h), rstd, h);
+                norm_load<T>(a, row, at, h);            // (H or Y may be X or the residual: a piece is read and written by one lane, here last)
+                if (a.H) store_piece<T>(static_cast<E *>(a.H) + row * a.h_ld, at, a.k, h);
+                gain_piece<T>(a, at, g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[e] *= g[e];
+                finish(row, at, encode(row, at, h), rstd, h);
             }
         }
     }
@@ -290,17 +295,20 @@ static void launch_norm(const NormArgs &a, int threads, hipStream_t st)
     hipLaunchKernelGGL(HIP_KERNEL_NAME(norm_kernel<T, NV, LONG>), dim3(grid), dim3((unsigned)threads), 0, st, a);
 }
 
+// Pieces per lane: one, the shortest way through a row (1 x 8192: 3.8 us, with two 4.0, with four 5.3); two where that would take more than
+// half of a compute unit's wavefronts for one row and there are rows for all of them (4096 x 8192: 59 us with one, 48 with two, 51 with four;
+// 512 x 8192: 9.0, 8.4, 9.2; 4096 x 4096 and 333 x 4100 are faster with one); more only where the row asks for them.
 template <class T>
 static void launch_norm_of(const NormArgs &a, hipStream_t st)
 {
     const int pieces = a.kb * 16;
-    auto waves = [&](int nv) { return (pieces + nv * kWave - 1) / (nv * kWave) * kWave; };
-    if (pieces <= 1024)
-        launch_norm<T, 1, false>(a, waves(1), st);
+    auto threads = [&](int nv) { return (pieces + nv * kWave - 1) / (nv * kWave) * kWave; };
+    if (pieces <= 512 || (pieces <= 1024 && a.m <= device_info().cus))
+        launch_norm<T, 1, false>(a, threads(1), st);
     else if (pieces <= 2048)
-        launch_norm<T, 2, false>(a, waves(2), st);
+        launch_norm<T, 2, false>(a, threads(2), st);
     else if (pieces <= 4096)
-        launch_norm<T, 4, false>(a, waves(4), st);
+        launch_norm<T, 4, false>(a, threads(4), st);
     else
         launch_norm<T, 1, true>(a, 1024, st);
 }

@@ -152,20 +152,30 @@ __global__ __launch_bounds__(1024) void block_stream_kernel(BlockGemmArgs a)
 }
 
 // ---- many tokens: tiles through LDS ----
-// A workgroup of WR x WT wavefronts has a tile of 16 AF WR rows x 16 BF WT tokens; STAGES buffers of 128 inputs are
-// filled by loads that write LDS directly, STAGES - 1 blocks ahead.  A wavefront waits until no more of its loads are under way than the later
-// blocks' pieces, which its pieces of this one are not among; the barrier after it makes that everyone's.  The tokens' scales are
-// fetched for four blocks at a time (they are next to one another), into two buffers of their own, with the pieces of the first of
-// the four: a wait that leaves out of account that those are more loads ends the later for it, never sooner.
+// A workgroup of WR x WT wavefronts has a tile of 16 AF WR rows x 16 BF WT tokens.  STAGES buffers of one block each are
+// filled by loads that write LDS directly.  There is one barrier per block, TAIL row fragments before its end, when a wavefront has read all it
+// needs of the block: past it everyone's pieces of the next block are there (each has waited for its own), so that the next
+// block's first fragments are read during the last products of this one, and this block's buffer is free to be filled.
+// The tokens' scales are fetched for 16 blocks at a time (64 bytes of a token's row), into two buffers of their own, ahead of the pieces of
+// the first of the 16.  A wavefront waits until no more of its loads are under way than the pieces of later blocks; that some of
+// those may be scales makes it wait longer, never shorter.
+// Results leave through LDS, so that a store instruction writes whole lines of a token's row.
+template <int BM, int BN, int STAGES>
+struct TileLds {
+    static constexpr int stage = (BM + BN) * kBlk, scales = STAGES * stage, chunk = BN * 64, bytes = scales + 2 * chunk;
+};
+
 template <int WR, int WT, int AF, int BF, int STAGES, bool EXACT, class T>
 __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmArgs a)
 {
-    constexpr int WAVES = WR * WT, BM = 16 * AF * WR, BN = 16 * BF * WT;
-    constexpr int WB = BM * kBlk, XB = BN * kBlk, SL = (BN + 63) / 64, SB = SL * 1024, STAGE = WB + XB, SCALES = STAGES * STAGE;
-    constexpr int WL = WB / 1024 / WAVES, XL = XB / 1024 / WAVES, LOADS = WL + XL;
-    static_assert(WL * WAVES * 1024 == WB && XL * WAVES * 1024 == XB && BM % kWTileRows == 0 && AF % 4 == 0, "tile");
+    typedef typename T::type E;
+    constexpr int WAVES = WR * WT, BM = 16 * AF * WR, BN = 16 * BF * WT, TAIL = AF / 4;
+    constexpr int WB = BM * kBlk, XB = BN * kBlk;
+    constexpr int WL = WB / 1024 / WAVES, XL = XB / 1024 / WAVES, SL = BN / 16 / WAVES, LOADS = WL + XL;
+    typedef TileLds<BM, BN, STAGES> Lds;
+    static_assert(WL * WAVES * 1024 == WB && XL * WAVES * 1024 == XB && SL * WAVES * 16 == BN && BM % kWTileRows == 0 && AF % 4 == 0, "tile");
     static_assert(AF * 16 == 64 || (AF * 16) % kBlk == 0, "a wavefront's rows have one scale per block");
-    static_assert(SL <= WAVES && STAGES <= 4, "scales");
+    static_assert(STAGES >= 2 && STAGES <= 8 && (int)(BM * BN * sizeof(E)) <= Lds::scales, "buffers");
     extern __shared__ __align__(16) uint8_t lds[];
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x & (kWave - 1);
     const int wr = w % WR, wt = w / WR, j = lane & 15, q = lane >> 4;
@@ -185,7 +195,7 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
 
     // this wavefront's shares of a block: pieces of a KiB of the weight tiles, and groups of eight tokens whose eight 16-byte pieces are put in another
     // order in each of eight rows, so that a fragment's reads find all banks
-    uint32_t woff[WL], xoff[XL];
+    uint32_t woff[WL], xoff[XL], soff[SL];
 #pragma unroll
     for (int i = 0; i < WL; ++i) {
         const int piece = w * WL + i;
@@ -193,14 +203,45 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     }
 #pragma unroll
     for (int i = 0; i < XL; ++i) xoff[i] = (uint32_t)((w * XL + i) * 8 + lane / 8) * kp + (uint32_t)((lane & 7) ^ (lane / 8)) * 16u;
-    const uint32_t soff = (uint32_t)(w * 64 + lane) * (uint32_t)a.kb * 4u;
-    auto fetch = [&](int b) {
-        const uint32_t base = lds0 + (uint32_t)(b % STAGES) * STAGE;
 #pragma unroll
-        for (int i = 0; i < WL; ++i) load_to_lds(wd, woff[i], (uint32_t)b * kWTileBytes, base + (uint32_t)(w * WL + i) * 1024u);
+    for (int i = 0; i < SL; ++i) soff[i] = (uint32_t)((w * SL + i) * 16 + lane / 4) * (uint32_t)a.kb * 4u + (uint32_t)((lane & 3) ^ (lane >> 4)) * 16u;
+    auto fetch_scales = [&](int b) {
 #pragma unroll
-        for (int i = 0; i < XL; ++i) load_to_lds(xd, xoff[i], (uint32_t)b * kBlk, base + WB + (uint32_t)(w * XL + i) * 1024u);
-        if ((b & 3) == 0 && w < SL) load_to_lds(sd, soff + (uint32_t)b * 4u, 0u, lds0 + SCALES + (uint32_t)(b >> 2 & 1) * SB + (uint32_t)w * 1024u);
+        for (int i = 0; i < SL; ++i)
+            load_to_lds(sd, soff[i] + (uint32_t)b * 4u, 0u, lds0 + Lds::scales + (uint32_t)(b >> 4 & 1) * Lds::chunk + (uint32_t)(w * SL + i) * 1024u);
+    };
+    // Piece `i` of this wavefront's of block b.  Past the last block nothing is read (an offset out of the buffer's range gives zeros): the number of
+    // loads under way is the same everywhere.
+    auto fetch_piece = [&](auto ic, int b, int buffer) {
+        constexpr int i = decltype(ic)::value;
+        const uint32_t base = lds0 + (uint32_t)buffer * Lds::stage, out = b < a.kb ? 0u : 0x80000000u, bb = b < a.kb ? (uint32_t)b : 0u;
+        if constexpr (i < WL)
+            load_to_lds(wd, woff[i] | out, bb * kWTileBytes, base + (uint32_t)(w * WL + i) * 1024u);
+        else
+            load_to_lds(xd, xoff[i - WL] | out, bb * kBlk, base + WB + (uint32_t)(w * XL + i - WL) * 1024u);
+    };
+
+    // The rows' scales of 64 blocks, one per lane.  They are waited for where they are loaded: a wait of the compiler's inside the loop would be
+    // for all the loads under way, which it does not know of.
+    float row_scales;
+    auto fetch_row_scales = [&](int b) {
+        row_scales = ws[min(b + lane, a.kb - 1)];
+        asm volatile("" : "+v"(row_scales));
+    };
+    fetch_row_scales(0);
+
+    const int xrow = (wt * BF * 16 + j) * kBlk, xp0 = (q ^ (j & 7)) * 16, xp1 = ((4 + q) ^ (j & 7)) * 16;
+    auto load_x = [&](int buffer, int t) {
+        const uint8_t *row = lds + buffer * Lds::stage + WB + xrow + t * 16 * kBlk;
+        return Codes<EXACT>(*reinterpret_cast<const uint4_t *>(row + xp0), *reinterpret_cast<const uint4_t *>(row + xp1));
+    };
+    auto load_w = [&](int buffer, int i) {
+        const uint8_t *frag = lds + buffer * Lds::stage + (wr * AF + i) * 2048 + lane * 16;
+        return Codes<EXACT>(*reinterpret_cast<const uint4_t *>(frag), *reinterpret_cast<const uint4_t *>(frag + 1024));
+    };
+    auto load_scale = [&](int b, int t) {
+        return *reinterpret_cast<const float *>(lds + Lds::scales + (b >> 4 & 1) * Lds::chunk + ((wt * BF + t) * 16 + j) * 64 +
+                                                ((b >> 2 & 3) ^ (j >> 2)) * 16 + (b & 3) * 4);
     };
 
     float4_t acc[AF][BF];
@@ -208,67 +249,123 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     for (int i = 0; i < AF; ++i)
 #pragma unroll
         for (int t = 0; t < BF; ++t) acc[i][t] = float4_t{0.f, 0.f, 0.f, 0.f};
+    // Row fragments in registers: two in turn, and the last TAIL, which are all read before the barrier, in their own.
+    constexpr int MAIN = AF - TAIL, WBUF = TAIL > 1 ? 2 + TAIL : 2;
+    auto place = [](int i) { return i < MAIN || TAIL == 1 ? i % 2 : 2 + i - MAIN; };
+    Codes<EXACT> x[BF], wv[WBUF];
+    float s[BF], wsb;
+    // The products of a block in order: fragment by fragment, the last TAIL token tile by token tile.  Each is added LAG products later, when the matrix
+    // pipe has it ready.
+    constexpr int SLOTS = AF * BF, LAG = EXACT ? 1 : 3;
+    // A block's pieces are asked for one at a time between the products, EARLY of them in the tail that follows the barrier and the others in the
+    // next block: all at once they held the wavefronts up behind one another, 600 of 3170 cycles per block of 256 x 256.
+    constexpr int SPREAD = 2, EARLY = TAIL * BF / SPREAD;
+    static_assert(EARLY <= LOADS && (LOADS - EARLY) * SPREAD <= MAIN * BF, "every piece has its place");
+    auto row_of = [](int n) { return n < MAIN * BF ? n / BF : MAIN + (n - MAIN * BF) % TAIL; };
+    auto token_of = [](int n) { return n < MAIN * BF ? n % BF : (n - MAIN * BF) / TAIL; };
+    float4_t p[LAG + 1];
+    auto add = [&](auto nc) {
+        constexpr int n = decltype(nc)::value, i = row_of(n), t = token_of(n);
 #pragma unroll
-    for (int b = 0; b < STAGES - 1; ++b)
-        if (b < a.kb) fetch(b);
+        for (int r = 0; r < 4; ++r) acc[i][t][r] = __builtin_fmaf(p[n % (LAG + 1)][r], s[t], acc[i][t][r]);
+    };
 
-    for (int b = 0; b < a.kb; ++b) {
-        const float wsb = ws[b];
-        if (b + STAGES - 2 < a.kb)
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"((STAGES - 2) * LOADS) : "memory");
-        else
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" : : : "memory");
-        // (everyone is past block b - 1, whose buffer this fills)
-        if (b + STAGES - 1 < a.kb) fetch(b + STAGES - 1);
-        const uint8_t *base = lds + (b % STAGES) * STAGE;
-        Codes<EXACT> x[BF];
-        float s[BF];
 #pragma unroll
-        for (int t = 0; t < BF; ++t) {
-            const int tok = (wt * BF + t) * 16 + j;
-            const uint8_t *row = base + WB + tok * kBlk;
-            x[t] = Codes<EXACT>(*reinterpret_cast<const uint4_t *>(row + ((q ^ (tok & 7)) * 16)),
-                                *reinterpret_cast<const uint4_t *>(row + (((4 + q) ^ (tok & 7)) * 16)));
-            s[t] = *reinterpret_cast<const float *>(lds + SCALES + (b >> 2 & 1) * SB + tok * 16 + (b & 3) * 4) * wsb;
-        }
-#pragma unroll
-        for (int i = 0; i < AF; ++i) {
-            const uint8_t *frag = base + (wr * AF + i) * 2048 + lane * 16;
-            const Codes<EXACT> wf(*reinterpret_cast<const uint4_t *>(frag), *reinterpret_cast<const uint4_t *>(frag + 1024));
-#pragma unroll
-            for (int t = 0; t < BF; ++t) {
-                const float4_t p = block_product(wf, x[t]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[i][t][r] = __builtin_fmaf(p[r], s[t], acc[i][t][r]);
-            }
-        }
+    for (int b = 0; b < STAGES - 1; ++b) {
+        if (b == 0) fetch_scales(0);
+        static_for<LOADS>([&](auto ic) { fetch_piece(ic, b, b); });
     }
+    static_for<EARLY>([&](auto ic) { fetch_piece(ic, STAGES - 1, STAGES - 1); });
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+    wsb = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, row_scales), 0));
 #pragma unroll
     for (int t = 0; t < BF; ++t) {
-        const int tok = tok0 + (wt * BF + t) * 16 + j;
-        if (tok < a.m) {
-            typename T::type *row = static_cast<typename T::type *>(a.Y) + tok * a.y_ld;
+        x[t] = load_x(0, t);
+        s[t] = load_scale(0, t) * wsb;
+    }
+    wv[0] = load_w(0, 0);
+
+    for (int b = 0, buffer = 0; b < a.kb; ++b) {
+        const int after = buffer + 1 < STAGES ? buffer + 1 : 0, before = buffer > 0 ? buffer - 1 : STAGES - 1;
+        static_for<MAIN * BF>([&](auto nc) {
+            constexpr int n = decltype(nc)::value, i = row_of(n), t = token_of(n);
+            if constexpr (t == 0) {
+                if constexpr (i + 1 < MAIN || TAIL == 1) wv[place(i + 1)] = load_w(buffer, i + 1);
+                if constexpr (TAIL > 1 && i >= MAIN - TAIL) wv[place(i + TAIL)] = load_w(buffer, i + TAIL);
+            }
+            if constexpr (n % SPREAD == 0 && EARLY + n / SPREAD < LOADS)
+                fetch_piece(std::integral_constant<int, EARLY + n / SPREAD>{}, b + STAGES - 1, before);
+            p[n % (LAG + 1)] = block_product(wv[place(i)], x[t]);
+            if constexpr (n >= LAG) add(std::integral_constant<int, n - LAG>{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        // The sums so far are made here: the compiler would put them off past the barrier, and spill the products.
 #pragma unroll
-            for (int u = 0; u < AF / 4; ++u) {
-                float y[16];
+        for (int i = 0; i < MAIN; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) y[e] = acc[4 * u + e / 4][t][e % 4];
-                const int o = o0 + (wr * AF / 4 + u) * kWTileRows + 16 * q;
-                if constexpr (sizeof(typename T::type) == 4) {
+            for (int t = 0; t < BF; ++t) asm volatile("" : "+v"(acc[i][t]));
+        if (((b + 1) & (kWave - 1)) == 0) fetch_row_scales(b + 1);
+        wsb = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, row_scales), (b + 1) & (kWave - 1)));
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"((STAGES - 2) * LOADS) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" : : : "memory");
+        if (((b + STAGES) & 15) == 0) fetch_scales(b + STAGES);
+        // (past the last block what is read is an older one's, and is not used)
+        float sn[BF];
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        const float z[4] = {y[e], y[e + 1], y[e + 2], y[e + 3]};
-                        store_piece<T>(row, o + e, a.n, z);
-                    }
-                } else {
+        for (int t = 0; t < BF; ++t) sn[t] = load_scale(b + 1, t);
+        wv[0] = load_w(after, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        static_for<TAIL * BF>([&](auto nc) {
+            constexpr int n = MAIN * BF + decltype(nc)::value, i = row_of(n), t = token_of(n);
+            if constexpr ((n - MAIN * BF) % SPREAD == 0)
+                fetch_piece(std::integral_constant<int, (n - MAIN * BF) / SPREAD>{}, b + STAGES, buffer);
+            p[n % (LAG + 1)] = block_product(wv[place(i)], x[t]);
+            if constexpr (i == AF - 1) x[t] = load_x(after, t);
+            add(std::integral_constant<int, n - LAG>{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        static_for<LAG>([&](auto nc) { add(std::integral_constant<int, SLOTS - LAG + decltype(nc)::value>{}); });
 #pragma unroll
-                    for (int e = 0; e < 16; e += 8) {
-                        const float z[8] = {y[e], y[e + 1], y[e + 2], y[e + 3], y[e + 4], y[e + 5], y[e + 6], y[e + 7]};
-                        store_piece<T>(row, o + e, a.n, z);
-                    }
-                }
+        for (int t = 0; t < BF; ++t) s[t] = sn[t] * wsb;
+        buffer = after;
+    }
+
+    // Results to LDS: a row of BM per token, its 16-byte pieces in another order in each of 16 rows; from there a piece per lane and store.
+    constexpr int PIECE = 16 / sizeof(E), PER_ROW = BM / PIECE;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+#pragma unroll
+    for (int t = 0; t < BF; ++t) {
+        const int tok = (wt * BF + t) * 16 + j;
+#pragma unroll
+        for (int u = 0; u < AF / 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; e += PIECE) {
+                typedef E vec __attribute__((ext_vector_type(PIECE)));
+                vec v;
+#pragma unroll
+                for (int z = 0; z < PIECE; ++z) v[z] = (E)acc[4 * u + (e + z) / 4][t][(e + z) % 4];
+                const int c = ((wr * AF / 4 + u) * kWTileRows + 16 * q + e) / PIECE;
+                *reinterpret_cast<vec *>(lds + (tok * PER_ROW + (c ^ (tok & 15))) * 16) = v;
+            }
+    }
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < toks * PER_ROW; i += WAVES * kWave) {
+        const int tok = i / PER_ROW, c = i % PER_ROW, o = o0 + c * PIECE;
+        if (o < a.n) {
+            typedef E vec __attribute__((ext_vector_type(PIECE)));
+            const vec v = *reinterpret_cast<const vec *>(lds + (tok * PER_ROW + (c ^ (tok & 15))) * 16);
+            E *row = static_cast<E *>(a.Y) + (int64_t)(tok0 + tok) * a.y_ld;
+            if (o + PIECE <= a.n) {
+                Piece<T, PIECE>::store_streaming(row + o, v);
+            } else {
+#pragma unroll
+                for (int z = 0; z < PIECE; ++z)
+                    if (o + z < a.n) row[o + z] = v[z];
             }
         }
     }
@@ -287,12 +384,14 @@ static void launch_stream(const BlockGemmArgs &a, hipStream_t st)
 template <int WR, int WT, int AF, int BF, int STAGES, bool EXACT, class T>
 static int launch_tile(BlockGemmArgs a, hipStream_t st)
 {
-    constexpr int BM = 16 * AF * WR, BN = 16 * BF * WT, LDS = STAGES * (BM + BN) * kBlk + (BN + 63) / 64 * 2048;
+    constexpr int BM = 16 * AF * WR, BN = 16 * BF * WT;
+    constexpr size_t LDS = TileLds<BM, BN, STAGES>::bytes;
     a.tiles_o = (int)(((int64_t)a.n + BM - 1) / BM);
     a.tiles_t = (int)(((int64_t)a.m + BN - 1) / BN);
     const int64_t tiles = (int64_t)a.tiles_o * a.tiles_t;
     if (tiles * (WR * WT * kWave) > UINT32_MAX) return SLIM_ERR_SHAPE;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(block_tile_kernel<WR, WT, AF, BF, STAGES, EXACT, T>), dim3((unsigned)tiles), dim3(WR * WT * kWave), LDS, st, a);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(block_tile_kernel<WR, WT, AF, BF, STAGES, EXACT, T>), dim3((unsigned)tiles), dim3(WR * WT * kWave), LDS,
+                       st, a);
     return SLIM_OK;
 }
 
