@@ -19,6 +19,9 @@ namespace slim {
 
 typedef int int8v_t __attribute__((ext_vector_type(8)));
 
+// fp32 behind a uniform address, read by scalar loads
+typedef __attribute__((address_space(4))) const float scalar_float;
+
 struct BlockGemmArgs {
     const uint8_t *W;        // tiles of 64 x 128
     const float *ws;         // [row blocks][kb]
@@ -74,67 +77,128 @@ __device__ __forceinline__ float4_t block_product(const Codes<false> &x, const C
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, float4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
 }
 
-// ---- few tokens: the weights are streamed once, each wavefront of a workgroup a share of the blocks ----
-// FR fragments of 16 rows and TB tiles of 16 tokens per workgroup.  Wavefront w takes blocks w, w + S, ...; the S partial results meet in LDS
-// and are added in order.
-template <int FR, int TB, class T>
-__global__ __launch_bounds__(1024) void block_stream_kernel(BlockGemmArgs a)
+// N load instructions of 64 x 16 bytes that write LDS, a KiB apart both in memory and in LDS: to byte lds_byte + AT (uniform) on, in lane order.
+// The compiler does not see the loads: the caller waits for them.
+template <int N, int AT>
+__device__ __forceinline__ void load_run_to_lds(rsrc_t r, uint32_t lane_off, uint32_t uniform_off, uint32_t lds_byte)
 {
-    extern __shared__ __align__(16) float4_t part[];       // [S][FR * TB][64]
-    constexpr int U = FR * TB >= 8 ? 1 : FR * TB >= 4 ? 2 : 4;
+    static_assert(N == 1 || N == 2 || N == 4, "run");
+    if constexpr (N == 1)
+        asm volatile("s_add_u32 m0, %3, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+                     :
+                     : "v"(lane_off), "s"(r), "s"(uniform_off), "s"(lds_byte), "n"(AT)
+                     : "memory", "scc", "m0");
+    else if constexpr (N == 2)
+        asm volatile("s_add_u32 m0, %3, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds\n\t"
+                     "buffer_load_dwordx4 %0, %1, %2 offen offset:1024 lds"
+                     :
+                     : "v"(lane_off), "s"(r), "s"(uniform_off), "s"(lds_byte), "n"(AT)
+                     : "memory", "scc", "m0");
+    else
+        asm volatile("s_add_u32 m0, %3, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds\n\t"
+                     "buffer_load_dwordx4 %0, %1, %2 offen offset:1024 lds\n\t"
+                     "buffer_load_dwordx4 %0, %1, %2 offen offset:2048 lds\n\t"
+                     "buffer_load_dwordx4 %0, %1, %2 offen offset:3072 lds"
+                     :
+                     : "v"(lane_off), "s"(r), "s"(uniform_off), "s"(lds_byte), "n"(AT)
+                     : "memory", "scc", "m0");
+}
+
+// ---- few tokens: the weights are streamed once, each wavefront of a workgroup a share of the blocks ----
+// FR fragments of 16 rows and TB tiles of 16 tokens per workgroup of S wavefronts, a run of blocks per wavefront.  A wavefront is a
+// pipeline of its own: D blocks' operands of its share are under way to its own part of LDS (loads that write LDS; the tokens' as eight rows of
+// 128 bytes per load, in the order of block_tile_kernel's: as a fragment needs them, 16 rows of 64, they take more than twice the time).
+// The S partial results meet in LDS and are added in order.
+template <int FR, int TB>
+struct StreamLds {
+    static constexpr int stage = (FR + TB) * 2048, scales = 2048;         // per wavefront: of a block; of twice four blocks
+    static constexpr size_t bytes(int waves, int depth)
+    {
+        const size_t ring = (size_t)waves * (depth * stage + scales), sums = (size_t)waves * FR * TB * kWave * sizeof(float4_t);
+        return ring > sums ? ring : sums;
+    }
+};
+
+template <int FR, int TB, int D, int THREADS, class T>
+__global__ __launch_bounds__(THREADS) void block_stream_kernel(BlockGemmArgs a)
+{
+    typedef StreamLds<FR, TB> Lds;
+    constexpr int LOADS = 2 * (FR + TB), RUN = FR > 1 ? 4 : 2;
+    extern __shared__ __align__(16) uint8_t lds[];
     const int S = (int)blockDim.x / kWave, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x & (kWave - 1);
     const int f0 = (int)blockIdx.x * FR, rt = f0 >> 2, t0 = f0 & 3, j = lane & 15, q = lane >> 4;
     const uint32_t kp = (uint32_t)a.kb * kBlk;
-    const uint8_t *W = a.W + (int64_t)rt * a.kb * kWTileBytes + t0 * 2048 + lane * 16;
-    const float *ws = a.ws + (int64_t)(rt >> 1) * a.kb;
+    const rsrc_t wd = make_rsrc(a.W + (int64_t)rt * a.kb * kWTileBytes, (uint32_t)a.kb * kWTileBytes);
     const rsrc_t xd = make_rsrc(a.X, (uint32_t)a.m * kp), sd = make_rsrc(a.xs, (uint32_t)a.m * (uint32_t)a.kb * 4u);
+    const scalar_float *ws = (const scalar_float *)(a.ws + (int64_t)(rt >> 1) * a.kb);
+    const int share = (a.kb + S - 1) / S, first = w * share, count = min(share, a.kb - first);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+    const uint32_t ring = (uint32_t)w * (D * Lds::stage), scales = (uint32_t)S * (D * Lds::stage) + (uint32_t)w * Lds::scales;
 
+    uint32_t xoff[2 * TB];
+#pragma unroll
+    for (int i = 0; i < 2 * TB; ++i) xoff[i] = (uint32_t)(8 * i + lane / 8) * kp + (uint32_t)((lane & 7) ^ (lane / 8)) * 16u;
+    const uint32_t woff = (uint32_t)t0 * 2048u + (uint32_t)lane * 16u, soff = (uint32_t)lane * (uint32_t)a.kb * 4u;
+    // The operands of the share's block i (past its end nothing: offsets out of range; the number of loads under way is what counts).
+    auto fetch = [&](int i, int slot) {
+        const uint32_t out = i < count ? 0u : 0x80000000u, b = i < count ? (uint32_t)(first + i) : 0u;
+        const uint32_t base = lds0 + ring + (uint32_t)slot * Lds::stage;
+        if ((i & 3) == 0) load_to_lds(sd, (soff + b * 4u) | out, 0u, lds0 + scales + (uint32_t)(i >> 2 & 1) * 1024u);
+#pragma unroll
+        for (int f = 0; f < 2 * FR; f += RUN) load_run_to_lds<RUN, 0>(wd, (woff + (uint32_t)f * 1024u) | out, b * kWTileBytes, base + (uint32_t)f * 1024u);
+#pragma unroll
+        for (int t = 0; t < 2 * TB; ++t) load_to_lds(xd, xoff[t] | out, b * kBlk, base + (uint32_t)(2 * FR + t) * 1024u);
+    };
     float4_t acc[FR][TB];
 #pragma unroll
     for (int f = 0; f < FR; ++f)
 #pragma unroll
         for (int t = 0; t < TB; ++t) acc[f][t] = float4_t{0.f, 0.f, 0.f, 0.f};
-
-    for (int b0 = w; b0 < a.kb; b0 += S * U) {
-        uint4_t wv[U][FR][2], xv[U][TB][2];
-        float s[U][TB];
+    if (count > 0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int b = b0 + u * S;
-            // blocks past the end: the last one again, with scale zero (a NaN among its codes is in the result anyway)
-            const int bc = b < a.kb ? b : a.kb - 1;
+        for (int i = 0; i < D; ++i) fetch(i, i);
+    }
+    // (the rows' scale comes by a scalar load, a block ahead: those are counted apart from the loads to LDS)
+    float wsb, next_wsb = ws[min(first, a.kb - 1)];
+    for (int i = 0, slot = 0; i < count; ++i) {
+        wsb = next_wsb;
+        next_wsb = ws[min(first + i + 1, a.kb - 1)];
+        asm volatile("s_waitcnt vmcnt(%0)" : : "n"((D - 1) * LOADS) : "memory");
+        const uint8_t *base = lds + ring + slot * Lds::stage;
+        uint4_t wv[FR][2], xv[TB][2];
+        float s[TB];
 #pragma unroll
-            for (int f = 0; f < FR; ++f)
+        for (int f = 0; f < FR; ++f)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    wv[u][f][h] = *reinterpret_cast<const uint4_t *>(W + (int64_t)bc * kWTileBytes + f * 2048 + h * 1024);
-            const float wsb = b < a.kb ? ws[bc] : 0.f;
+            for (int h = 0; h < 2; ++h) wv[f][h] = *reinterpret_cast<const uint4_t *>(base + (2 * f + h) * 1024 + lane * 16);
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                xv[t][h] = *reinterpret_cast<const uint4_t *>(base + FR * 2048 + (16 * t + j) * kBlk + (((4 * h + q) ^ (j & 7)) * 16));
+            s[t] = *reinterpret_cast<const float *>(lds + scales + (i >> 2 & 1) * 1024 + (16 * t + j) * 16 + (i & 3) * 4) * wsb;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        fetch(i + D, slot);
+        slot = slot + 1 < D ? slot + 1 : 0;
+        Codes<true> x[TB];
+#pragma unroll
+        for (int t = 0; t < TB; ++t) x[t] = Codes<true>(xv[t][0], xv[t][1]);
+#pragma unroll
+        for (int f = 0; f < FR; ++f) {
+            const Codes<true> wf(wv[f][0], wv[f][1]);
 #pragma unroll
             for (int t = 0; t < TB; ++t) {
-                const uint32_t row = (uint32_t)(t * 16 + j);
+                const float4_t p = block_product(wf, x[t]);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) xv[u][t][h] = load16(xd, row * kp + (uint32_t)q * 16u, (uint32_t)bc * kBlk + (uint32_t)h * 64u);
-                const uint32_t sv = __builtin_amdgcn_raw_buffer_load_b32(sd, (int)((row * (uint32_t)a.kb + (uint32_t)bc) * 4u), 0, 0);
-                s[u][t] = __builtin_bit_cast(float, sv) * wsb;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            Codes<true> x[TB];
-#pragma unroll
-            for (int t = 0; t < TB; ++t) x[t] = Codes<true>(xv[u][t][0], xv[u][t][1]);
-#pragma unroll
-            for (int f = 0; f < FR; ++f) {
-                const Codes<true> wf(wv[u][f][0], wv[u][f][1]);
-#pragma unroll
-                for (int t = 0; t < TB; ++t) {
-                    const float4_t p = block_product(wf, x[t]);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[f][t][r] = __builtin_fmaf(p[r], s[u][t], acc[f][t][r]);
-                }
+                for (int r = 0; r < 4; ++r) acc[f][t][r] = __builtin_fmaf(p[r], s[t], acc[f][t][r]);
             }
         }
     }
+    // (nothing is under way into LDS, and no one reads operands there, when the sums go in)
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    __syncthreads();
+    float4_t *part = reinterpret_cast<float4_t *>(lds);                   // [S][FR * TB][64]
 #pragma unroll
     for (int f = 0; f < FR; ++f)
 #pragma unroll
@@ -169,9 +233,10 @@ template <int WR, int WT, int AF, int BF, int STAGES, bool EXACT, class T>
 __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmArgs a)
 {
     typedef typename T::type E;
-    constexpr int WAVES = WR * WT, BM = 16 * AF * WR, BN = 16 * BF * WT, TAIL = AF / 4;
+    constexpr int WAVES = WR * WT, BM = 16 * AF * WR, BN = 16 * BF * WT, TAIL = 2;
     constexpr int WB = BM * kBlk, XB = BN * kBlk;
     constexpr int WL = WB / 1024 / WAVES, XL = XB / 1024 / WAVES, SL = BN / 16 / WAVES, LOADS = WL + XL;
+    constexpr int RUN = EXACT && WL >= 4 ? 4 : WL < 4 ? WL : 1, WU = WL / RUN, UNITS = WU + XL;          // loads of weights in one go, and units of loads per block
     typedef TileLds<BM, BN, STAGES> Lds;
     static_assert(WL * WAVES * 1024 == WB && XL * WAVES * 1024 == XB && SL * WAVES * 16 == BN && BM % kWTileRows == 0 && AF % 4 == 0, "tile");
     static_assert(AF * 16 == 64 || (AF * 16) % kBlk == 0, "a wavefront's rows have one scale per block");
@@ -185,40 +250,43 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     const int o0 = tile % a.tiles_o * BM, tok0 = tile / a.tiles_o * BN;
     const uint32_t kp = (uint32_t)a.kb * kBlk;
     const int rows = min(BM, (a.n - o0 + kWTileRows - 1) / kWTileRows * kWTileRows), toks = min(BN, a.m - tok0);
-    const rsrc_t wd = make_rsrc(a.W + (int64_t)o0 * kp, (uint32_t)rows * kp);
-    const rsrc_t xd = make_rsrc(a.X + (int64_t)tok0 * kp, (uint32_t)toks * kp);
+    const uint8_t *wbase = a.W + (int64_t)o0 * kp, *xbase = a.X + (int64_t)tok0 * kp;
     const rsrc_t sd = make_rsrc(a.xs + (int64_t)tok0 * a.kb, (uint32_t)toks * (uint32_t)a.kb * 4u);
     // rows past the layer's last block of 128 are zeros: any scale will do
     const int rb = min((o0 + wr * AF * 16) / kBlk, (a.n - 1) / kBlk);
     const float *ws = a.ws + (int64_t)rb * a.kb;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
 
-    // this wavefront's shares of a block: pieces of a KiB of the weight tiles, and groups of eight tokens whose eight 16-byte pieces are put in another
+    // this wavefront's shares of a block: a run of KiB of the weight tiles, and groups of eight tokens whose eight 16-byte pieces are put in another
     // order in each of eight rows, so that a fragment's reads find all banks
-    uint32_t woff[WL], xoff[XL], soff[SL];
+    uint32_t woff[WU], xoff[XL], soff[SL];
 #pragma unroll
-    for (int i = 0; i < WL; ++i) {
-        const int piece = w * WL + i;
+    for (int i = 0; i < WU; ++i) {
+        const int piece = w * WL + i * RUN;
         woff[i] = (uint32_t)(piece / 8) * (uint32_t)a.kb * kWTileBytes + (uint32_t)(piece % 8) * 1024u + (uint32_t)lane * 16u;
     }
 #pragma unroll
     for (int i = 0; i < XL; ++i) xoff[i] = (uint32_t)((w * XL + i) * 8 + lane / 8) * kp + (uint32_t)((lane & 7) ^ (lane / 8)) * 16u;
 #pragma unroll
-    for (int i = 0; i < SL; ++i) soff[i] = (uint32_t)((w * SL + i) * 16 + lane / 4) * (uint32_t)a.kb * 4u + (uint32_t)((lane & 3) ^ (lane >> 4)) * 16u;
+    for (int i = 0; i < SL; ++i)
+        soff[i] = (uint32_t)((w * SL + i) * 16 + lane / 4) * (uint32_t)a.kb * 4u + (uint32_t)((lane & 3) ^ (lane >> 4)) * 16u;
     auto fetch_scales = [&](int b) {
 #pragma unroll
         for (int i = 0; i < SL; ++i)
             load_to_lds(sd, soff[i] + (uint32_t)b * 4u, 0u, lds0 + Lds::scales + (uint32_t)(b >> 4 & 1) * Lds::chunk + (uint32_t)(w * SL + i) * 1024u);
     };
-    // Piece `i` of this wavefront's of block b.  Past the last block nothing is read (an offset out of the buffer's range gives zeros): the number of
+    // Unit `u` of this wavefront's share of block b.  Past the last block nothing is read (from a buffer of no length; zeros): the number of
     // loads under way is the same everywhere.
-    auto fetch_piece = [&](auto ic, int b, int buffer) {
-        constexpr int i = decltype(ic)::value;
-        const uint32_t base = lds0 + (uint32_t)buffer * Lds::stage, out = b < a.kb ? 0u : 0x80000000u, bb = b < a.kb ? (uint32_t)b : 0u;
-        if constexpr (i < WL)
-            load_to_lds(wd, woff[i] | out, bb * kWTileBytes, base + (uint32_t)(w * WL + i) * 1024u);
-        else
-            load_to_lds(xd, xoff[i - WL] | out, bb * kBlk, base + WB + (uint32_t)(w * XL + i - WL) * 1024u);
+    auto fetch_unit = [&](auto uc, int b, int buffer) {
+        constexpr int u = decltype(uc)::value;
+        const uint32_t base = lds0 + (uint32_t)buffer * Lds::stage;
+        if constexpr (u < WU) {
+            const rsrc_t d = make_rsrc(wbase, b < a.kb ? (uint32_t)rows * kp : 0u);
+            load_run_to_lds<RUN, u * RUN * 1024>(d, woff[u], (uint32_t)b * kWTileBytes, base + (uint32_t)(w * WL) * 1024u);
+        } else {
+            const rsrc_t d = make_rsrc(xbase, b < a.kb ? (uint32_t)toks * kp : 0u);
+            load_run_to_lds<1, WB + (u - WU) * 1024>(d, xoff[u - WU], (uint32_t)b * kBlk, base + (uint32_t)(w * XL) * 1024u);
+        }
     };
 
     // The rows' scales of 64 blocks, one per lane.  They are waited for where they are loaded: a wait of the compiler's inside the loop would be
@@ -257,10 +325,10 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     // The products of a block in order: fragment by fragment, the last TAIL token tile by token tile.  Each is added LAG products later, when the matrix
     // pipe has it ready.
     constexpr int SLOTS = AF * BF, LAG = EXACT ? 1 : 3;
-    // A block's pieces are asked for one at a time between the products, EARLY of them in the tail that follows the barrier and the others in the
+    // A block's loads are asked for a few at a time between the products, EARLY units of them in the tail that follows the barrier and the others in the
     // next block: all at once they held the wavefronts up behind one another, 600 of 3170 cycles per block of 256 x 256.
-    constexpr int SPREAD = 2, EARLY = TAIL * BF / SPREAD;
-    static_assert(EARLY <= LOADS && (LOADS - EARLY) * SPREAD <= MAIN * BF, "every piece has its place");
+    constexpr int SPREAD = SLOTS >= 2 * UNITS ? 2 : 1, EARLY = UNITS < (TAIL * BF + SPREAD - 1) / SPREAD ? UNITS : (TAIL * BF + SPREAD - 1) / SPREAD;
+    static_assert((UNITS - EARLY) * SPREAD <= MAIN * BF, "every unit has its place");
     auto row_of = [](int n) { return n < MAIN * BF ? n / BF : MAIN + (n - MAIN * BF) % TAIL; };
     auto token_of = [](int n) { return n < MAIN * BF ? n % BF : (n - MAIN * BF) / TAIL; };
     float4_t p[LAG + 1];
@@ -273,9 +341,9 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
 #pragma unroll
     for (int b = 0; b < STAGES - 1; ++b) {
         if (b == 0) fetch_scales(0);
-        static_for<LOADS>([&](auto ic) { fetch_piece(ic, b, b); });
+        static_for<UNITS>([&](auto uc) { fetch_unit(uc, b, b); });
     }
-    static_for<EARLY>([&](auto ic) { fetch_piece(ic, STAGES - 1, STAGES - 1); });
+    static_for<EARLY>([&](auto uc) { fetch_unit(uc, STAGES - 1, STAGES - 1); });
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
@@ -295,8 +363,8 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
                 if constexpr (i + 1 < MAIN || TAIL == 1) wv[place(i + 1)] = load_w(buffer, i + 1);
                 if constexpr (TAIL > 1 && i >= MAIN - TAIL) wv[place(i + TAIL)] = load_w(buffer, i + TAIL);
             }
-            if constexpr (n % SPREAD == 0 && EARLY + n / SPREAD < LOADS)
-                fetch_piece(std::integral_constant<int, EARLY + n / SPREAD>{}, b + STAGES - 1, before);
+            if constexpr (n % SPREAD == 0 && EARLY + n / SPREAD < UNITS)
+                fetch_unit(std::integral_constant<int, EARLY + n / SPREAD>{}, b + STAGES - 1, before);
             p[n % (LAG + 1)] = block_product(wv[place(i)], x[t]);
             if constexpr (n >= LAG) add(std::integral_constant<int, n - LAG>{});
             __builtin_amdgcn_sched_barrier(0);
@@ -320,8 +388,8 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
         __builtin_amdgcn_sched_barrier(0);
         static_for<TAIL * BF>([&](auto nc) {
             constexpr int n = MAIN * BF + decltype(nc)::value, i = row_of(n), t = token_of(n);
-            if constexpr ((n - MAIN * BF) % SPREAD == 0)
-                fetch_piece(std::integral_constant<int, (n - MAIN * BF) / SPREAD>{}, b + STAGES, buffer);
+            if constexpr ((n - MAIN * BF) % SPREAD == 0 && (n - MAIN * BF) / SPREAD < EARLY)
+                fetch_unit(std::integral_constant<int, (n - MAIN * BF) / SPREAD>{}, b + STAGES, buffer);
             p[n % (LAG + 1)] = block_product(wv[place(i)], x[t]);
             if constexpr (i == AF - 1) x[t] = load_x(after, t);
             add(std::integral_constant<int, n - LAG>{});
@@ -333,8 +401,8 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
         buffer = after;
     }
 
-    // Results to LDS: a row of BM per token, its 16-byte pieces in another order in each of 16 rows; from there a piece per lane and store.
-    constexpr int PIECE = 16 / sizeof(E), PER_ROW = BM / PIECE;
+    // Results to LDS: a row of BM per token, its 16-byte pieces in another order in each of up to 16 rows; from there a piece per lane and store.
+    constexpr int PIECE = 16 / sizeof(E), PER_ROW = BM / PIECE, TURN = (PER_ROW < 16 ? PER_ROW : 16) - 1;
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
@@ -350,7 +418,7 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
 #pragma unroll
                 for (int z = 0; z < PIECE; ++z) v[z] = (E)acc[4 * u + (e + z) / 4][t][(e + z) % 4];
                 const int c = ((wr * AF / 4 + u) * kWTileRows + 16 * q + e) / PIECE;
-                *reinterpret_cast<vec *>(lds + (tok * PER_ROW + (c ^ (tok & 15))) * 16) = v;
+                *reinterpret_cast<vec *>(lds + (tok * PER_ROW + (c ^ (tok & TURN))) * 16) = v;
             }
     }
     __syncthreads();
@@ -358,7 +426,7 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
         const int tok = i / PER_ROW, c = i % PER_ROW, o = o0 + c * PIECE;
         if (o < a.n) {
             typedef E vec __attribute__((ext_vector_type(PIECE)));
-            const vec v = *reinterpret_cast<const vec *>(lds + (tok * PER_ROW + (c ^ (tok & 15))) * 16);
+            const vec v = *reinterpret_cast<const vec *>(lds + (tok * PER_ROW + (c ^ (tok & TURN))) * 16);
             E *row = static_cast<E *>(a.Y) + (int64_t)(tok0 + tok) * a.y_ld;
             if (o + PIECE <= a.n) {
                 Piece<T, PIECE>::store_streaming(row + o, v);
@@ -371,14 +439,37 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     }
 }
 
+// S wavefronts, two blocks under way each: more of either was slower from 4096 rows on (28672 x 8192 at one token: 41 us with 4 or 8
+// wavefronts of one fragment, 52 with 16; three or four blocks under way 44 to 50).
 template <int FR, int TB, class T>
-static void launch_stream(const BlockGemmArgs &a, hipStream_t st)
+static void launch_stream(const BlockGemmArgs &a, int waves, hipStream_t st)
 {
-    const int most = FR * TB >= 16 ? 4 : FR * TB >= 8 ? 8 : 16;          // 64 KiB of partial results at most
-    const int waves = a.kb < most ? a.kb : most;
-    const unsigned grid = (unsigned)(wtile_rows(a.n) * 4 / FR);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(block_stream_kernel<FR, TB, T>), dim3(grid), dim3((unsigned)(waves * kWave)),
-                       (size_t)waves * FR * TB * kWave * sizeof(float4_t), st, a);
+    constexpr int D = 2, THREADS = 8 * kWave;
+    while (waves > 1 && StreamLds<FR, TB>::bytes(waves, D) > device_info().lds) waves /= 2;
+    if (waves > a.kb) waves = a.kb;
+    const size_t lds = StreamLds<FR, TB>::bytes(waves, D);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(block_stream_kernel<FR, TB, D, THREADS, T>), dim3((unsigned)(wtile_rows(a.n) * 4 / FR)),
+                       dim3((unsigned)(waves * kWave)), lds, st, a);
+}
+
+// As many fragments per workgroup as leave 160 workgroups: the tokens are read once per workgroup, and four fragments are a whole tile of weights.
+// us with one / two / four fragments: 28672 x 8192 at 16 tokens 49 / 51 / 45, at 64 tokens 96 / 72 / 58; 8192 x 8192 at 64 tokens 23 / 19 / 22;
+// 5120 x 5120 at 48 tokens 11.9 / 9.9 / 13.8; 4096 x 4096 at 32 tokens 6.9 / 7.3 / 9.2.  Two fragments are not worth it for up to 16 tokens
+// (8192 x 8192: 12.2 / 15.1 / 13.0).
+template <int TB, class T>
+static void launch_stream_of(const BlockGemmArgs &a, hipStream_t st)
+{
+    const int fragments = wtile_rows(a.n) * 4;
+    if (fragments >= 4 * 160) {
+        launch_stream<4, TB, T>(a, 4, st);
+        return;
+    }
+    if constexpr (TB > 1)
+        if (fragments >= 2 * 160) {
+            launch_stream<2, TB, T>(a, 4, st);
+            return;
+        }
+    launch_stream<1, TB, T>(a, fragments < 256 ? 8 : 4, st);
 }
 
 template <int WR, int WT, int AF, int BF, int STAGES, bool EXACT, class T>
@@ -395,27 +486,65 @@ static int launch_tile(BlockGemmArgs a, hipStream_t st)
     return SLIM_OK;
 }
 
+// Tiles of block_tile_kernel: rows, tokens, workgroups per compute unit (by LDS), and the time per block of 128 inputs with every compute unit
+// at work and with at most half of them (less power, less traffic).  The times (us) are those of single rounds on 4096 to
+// 11008 inputs; a call takes rounds * (blocks * time + 3) or so, and the tile with the least of that is taken.  The smaller tiles
+// are bound by the instructions a wavefront issues per block (its 32 additions per 8 products first of all), 256 x 256 by power.
+struct TileShape {
+    int rows, toks, per_cu;
+    float full, half;
+};
+constexpr TileShape kTiles[] = {{256, 256, 1, 1.7f, 1.3f}, {256, 128, 1, 1.0f, 0.8f}, {128, 128, 1, 0.62f, 0.5f},
+                                {64, 128, 1, 0.40f, 0.38f}, {64, 64, 2, 0.45f, 0.33f}};
+constexpr TileShape kExactTiles[] = {{128, 128, 2, 1.6f, 1.2f}, {128, 128, 1, 1.17f, 1.1f}, {64, 64, 2, 0.76f, 0.53f}};
+
+static int plan_tile(const BlockGemmArgs &a, bool exact)
+{
+    const TileShape *shapes = exact ? kExactTiles : kTiles;
+    const int count = exact ? (int)(sizeof kExactTiles / sizeof kExactTiles[0]) : (int)(sizeof kTiles / sizeof kTiles[0]);
+    const double cus = device_info().cus;
+    int best = 0;
+    double least = 0;
+    for (int i = 0; i < count; ++i) {
+        const TileShape &t = shapes[i];
+        const double tiles = (double)(((int64_t)a.n + t.rows - 1) / t.rows) * (double)(((int64_t)a.m + t.toks - 1) / t.toks);
+        const double rounds = __builtin_ceil(tiles / (cus * t.per_cu));
+        const double time = rounds * (a.kb * (2 * tiles <= cus * t.per_cu ? t.half : t.full) + 3.0);
+        if (i == 0 || time < least) {
+            least = time;
+            best = i;
+        }
+    }
+    return best;
+}
+
 template <class T>
 static int launch_block_gemm(const BlockGemmArgs &a, hipStream_t st)
 {
-    if (a.m <= 16) {
-        if (a.n <= 8192)
-            launch_stream<1, 1, T>(a, st);
-        else
-            launch_stream<4, 1, T>(a, st);
-        return SLIM_OK;
-    }
-    if (a.m <= 64) {
-        if (a.m <= 32)
-            launch_stream<2, 2, T>(a, st);
-        else
-            launch_stream<2, 4, T>(a, st);
-        return SLIM_OK;
+    switch ((a.m + 15) / 16) {
+    case 1: launch_stream_of<1, T>(a, st); return SLIM_OK;
+    case 2: launch_stream_of<2, T>(a, st); return SLIM_OK;
+    case 3: launch_stream_of<3, T>(a, st); return SLIM_OK;
+    case 4: launch_stream_of<4, T>(a, st); return SLIM_OK;
+    default: break;
     }
     constexpr bool EXACT = sizeof(typename T::type) == 4;
-    if constexpr (!EXACT)
-        if ((int64_t)((a.n + 255) / 256) * ((a.m + 255) / 256) >= 256) return launch_tile<2, 4, 8, 4, 2, false, T>(a, st);
-    return launch_tile<2, 2, 4, 4, 2, EXACT, T>(a, st);
+    const int shape = plan_tile(a, EXACT);
+    if constexpr (EXACT) {
+        switch (shape) {
+        case 0: return launch_tile<2, 2, 4, 4, 2, true, T>(a, st);
+        case 1: return launch_tile<2, 4, 4, 2, 4, true, T>(a, st);
+        default: return launch_tile<1, 4, 4, 1, 4, true, T>(a, st);
+        }
+    } else {
+        switch (shape) {
+        case 0: return launch_tile<2, 4, 8, 4, 2, false, T>(a, st);
+        case 1: return launch_tile<4, 2, 4, 4, 3, false, T>(a, st);
+        case 2: return launch_tile<2, 4, 4, 2, 4, false, T>(a, st);
+        case 3: return launch_tile<1, 4, 4, 2, 4, false, T>(a, st);
+        default: return launch_tile<1, 4, 4, 1, 4, false, T>(a, st);
+        }
+    }
 }
 
 }  // namespace slim
