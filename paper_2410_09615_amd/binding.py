@@ -582,29 +582,36 @@ ACTS = {"none": 0, "silu": 1}
 _E4M3 = torch.float8_e4m3fn
 
 
-def _matrix(t: torch.Tensor, like: torch.Tensor, name: str, shape=None, dtype=None):
-    """t's row stride; a matrix of whole rows on like's device, whatever lies between them."""
-    if not t.is_cuda or t.device != like.device:
-        raise ValueError(f"{name} must be on the inputs' device")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or t.dtype != (dtype or like.dtype):
-        raise ValueError(f"{name} must be a {dtype or like.dtype} matrix with contiguous rows")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {tuple(shape)}")
-    ld = t.stride(0)
-    # (the stride of a single row says nothing)
-    return ld if t.shape[0] > 1 else max(ld, t.shape[1])
+# A call on one token is a few microseconds and every look at a tensor a twentieth of one: each argument is looked at once.
+def _rows(t: torch.Tensor, name: str, dtype, shape, device: int) -> int:
+    """t's row stride; t is a matrix of `shape` (None: any) and `dtype` on `device`, whose rows have no gaps, whatever lies between them."""
+    at = t.get_device()
+    if at < 0 or at != device:
+        raise ValueError(f"{name} must be a device tensor on the inputs' device")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}")
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must be a matrix" + (f" of {tuple(shape)}" if shape is not None else ""))
+    ld, step = t.stride()
+    m, k = t.shape
+    if step != 1 and k > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return ld if m > 1 else max(ld, k)                # (the stride of a single row says nothing)
+
+
+def _whole(t: torch.Tensor, name: str, dtype, count: int, device: int) -> int:
+    """t's address; t has `count` elements of `dtype` on `device`, without gaps."""
+    if t.dtype is not dtype or t.numel() != count or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be {count} contiguous {dtype} on the inputs' device")
+    return t.data_ptr()
 
 
 def _code_buffers(m: int, k: int, codes, scales, device):
     kb = (k + 127) // 128
     if codes is None:
         codes = torch.empty(m, kb * 128, dtype=torch.uint8, device=device)
-    elif codes.dtype not in (torch.uint8, _E4M3) or codes.numel() != m * kb * 128 or codes.device != device or not codes.is_contiguous():
-        raise ValueError("codes must be contiguous uint8 [m][128 ceil(k / 128)] on the inputs' device")
     if scales is None:
         scales = torch.empty(m, kb, dtype=torch.float32, device=device)
-    elif scales.dtype != torch.float32 or scales.numel() != m * kb or scales.device != device or not scales.is_contiguous():
-        raise ValueError("scales must be contiguous float32 [m][ceil(k / 128)] on the inputs' device")
     return codes, scales
 
 
@@ -613,30 +620,37 @@ def slim_block_fp8_norm(X: torch.Tensor, gain: torch.Tensor | None = None, eps: 
     """h = X + residual, y = h gain / sqrt(mean(h^2) + eps) -> (codes uint8 [m][128 kb], scales fp32 [m][kb], H, Y): y in 8 bits with a
     scale per 128 inputs.  H, Y: True for a new matrix of X's type, or one to write (X or residual itself, for in place);
     None (returned as such): not wanted.  X, residual, H, Y fp16 or bf16 with any row stride; gain of X's type or fp32."""
-    if X.dtype not in (torch.float16, torch.bfloat16) or X.dim() != 2:
-        raise ValueError("X must be a float16 or bfloat16 matrix")
-    x_ld = _matrix(X, X, "X")
-    m, k = X.shape
+    device, dtype, shape = X.get_device(), X.dtype, X.shape
+    if dtype is not torch.float16 and dtype is not torch.bfloat16:
+        raise ValueError("X must be float16 or bfloat16")
+    x_ld = _rows(X, "X", dtype, None, device)
+    m, k = shape
+    kb = (k + 127) // 128
     r_ld = h_ld = y_ld = 0
     rp = hp = yp = gp = None
-    gt = DTYPES[X.dtype]
+    xt = gt = DTYPES[dtype]
     if residual is not None:
-        r_ld, rp = _matrix(residual, X, "residual", X.shape), residual.data_ptr()
+        r_ld, rp = _rows(residual, "residual", dtype, shape, device), residual.data_ptr()
     if gain is not None:
-        if gain.numel() != k or gain.dtype not in (X.dtype, torch.float32) or gain.device != X.device or not gain.is_contiguous():
-            raise ValueError("gain must be contiguous [k] of X's type or float32 on X's device")
-        gp, gt = gain.data_ptr(), DTYPES[gain.dtype]
-    if H is True:
-        H = torch.empty(m, k, dtype=X.dtype, device=X.device)
-    if Y is True:
-        Y = torch.empty(m, k, dtype=X.dtype, device=X.device)
+        gd = gain.dtype
+        if gd is torch.float32:
+            gt = 2
+        elif gd is not dtype:
+            raise ValueError("gain must be of X's type or float32")
+        gp = _whole(gain, "gain", gd, k, device)
     if H is not None:
-        h_ld, hp = _matrix(H, X, "H", X.shape), H.data_ptr()
+        if H is True:
+            H = torch.empty(m, k, dtype=dtype, device=X.device)
+        h_ld, hp = _rows(H, "H", dtype, shape, device), H.data_ptr()
     if Y is not None:
-        y_ld, yp = _matrix(Y, X, "Y", X.shape), Y.data_ptr()
-    codes, scales = _code_buffers(m, k, codes, scales, X.device)
-    status = lib().slim_block_fp8_norm(X.data_ptr(), x_ld, rp, r_ld, gp, gt, DTYPES[X.dtype], m, k, eps, hp, h_ld, yp, y_ld, codes.data_ptr(),
-                                       scales.data_ptr(), torch._C._cuda_getCurrentRawStream(X.device.index))
+        if Y is True:
+            Y = torch.empty(m, k, dtype=dtype, device=X.device)
+        y_ld, yp = _rows(Y, "Y", dtype, shape, device), Y.data_ptr()
+    if codes is None or scales is None:
+        codes, scales = _code_buffers(m, k, codes, scales, X.device)
+    status = lib().slim_block_fp8_norm(X.data_ptr(), x_ld, rp, r_ld, gp, gt, xt, m, k, eps, hp, h_ld, yp, y_ld,
+                                       _whole(codes, "codes", torch.uint8, m * kb * 128, device),
+                                       _whole(scales, "scales", torch.float32, m * kb, device), torch._C._cuda_getCurrentRawStream(device))
     if status != SLIM_OK:
         _check("slim_block_fp8_norm", status)
     return codes, scales, H, Y
@@ -645,16 +659,20 @@ def slim_block_fp8_norm(X: torch.Tensor, gain: torch.Tensor | None = None, eps: 
 def slim_block_fp8_act(G: torch.Tensor, U: torch.Tensor | None = None, act: str = "silu", codes=None, scales=None):
     """act(G) * U ("silu" or "none"; U None: act(G)) -> (codes uint8 [m][128 kb], scales fp32 [m][kb]).  G, U fp16 or bf16 [m][k] with any
     row stride: the halves of one product's output, for one.  act="none" without U quantizes an input as it is."""
-    if G.dtype not in (torch.float16, torch.bfloat16) or G.dim() != 2:
-        raise ValueError("G must be a float16 or bfloat16 matrix")
+    device, dtype, shape = G.get_device(), G.dtype, G.shape
+    if dtype is not torch.float16 and dtype is not torch.bfloat16:
+        raise ValueError("G must be float16 or bfloat16")
     if act not in ACTS:
         raise ValueError("act is 'silu' or 'none'")
-    g_ld = _matrix(G, G, "G")
-    m, k = G.shape
-    u_ld, up = (0, None) if U is None else (_matrix(U, G, "U", G.shape), U.data_ptr())
-    codes, scales = _code_buffers(m, k, codes, scales, G.device)
-    status = lib().slim_block_fp8_act(G.data_ptr(), g_ld, up, u_ld, ACTS[act], DTYPES[G.dtype], m, k, codes.data_ptr(), scales.data_ptr(),
-                                      torch._C._cuda_getCurrentRawStream(G.device.index))
+    g_ld = _rows(G, "G", dtype, None, device)
+    m, k = shape
+    kb = (k + 127) // 128
+    u_ld, up = (0, None) if U is None else (_rows(U, "U", dtype, shape, device), U.data_ptr())
+    if codes is None or scales is None:
+        codes, scales = _code_buffers(m, k, codes, scales, G.device)
+    status = lib().slim_block_fp8_act(G.data_ptr(), g_ld, up, u_ld, ACTS[act], DTYPES[dtype], m, k,
+                                      _whole(codes, "codes", torch.uint8, m * kb * 128, device),
+                                      _whole(scales, "scales", torch.float32, m * kb, device), torch._C._cuda_getCurrentRawStream(device))
     if status != SLIM_OK:
         _check("slim_block_fp8_act", status)
     return codes, scales
@@ -668,19 +686,18 @@ def slim_block_fp8_weight_sizes(n: int, k: int) -> dict:
 
 def slim_block_fp8_weight(W: torch.Tensor, codes=None, scales=None):
     """W [n][k] fp32, fp16 or bf16 (any row stride) -> (codes uint8 in tiles, flat; scales fp32 [ceil(n / 128)][ceil(k / 128)])."""
-    if W.dtype not in DTYPES or W.dim() != 2:
-        raise ValueError("W must be a float32, float16 or bfloat16 matrix")
-    ld = _matrix(W, W, "W")
+    if W.dtype not in DTYPES:
+        raise ValueError("W must be float32, float16 or bfloat16")
+    ld = _rows(W, "W", W.dtype, None, W.get_device())
     n, k = W.shape
     size = slim_block_fp8_weight_sizes(n, k)
     if codes is None:
         codes = torch.empty(size["codes"], dtype=torch.uint8, device=W.device)
     if scales is None:
         scales = torch.empty((n + 127) // 128, (k + 127) // 128, dtype=torch.float32, device=W.device)
-    for t, dt, name in ((codes, torch.uint8, "codes"), (scales, torch.float32, "scales")):
-        if t.dtype != dt or t.numel() * t.element_size() != size[name] or t.device != W.device or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous {dt} of slim_block_fp8_weight_sizes on W's device")
-    _check("slim_block_fp8_weight", lib().slim_block_fp8_weight(_ptr(W), ld, DTYPES[W.dtype], n, k, _ptr(codes), _ptr(scales), _stream(W)))
+    cp = _whole(codes, "codes", torch.uint8, size["codes"], W.get_device())
+    sp = _whole(scales, "scales", torch.float32, size["scales"] // 4, W.get_device())
+    _check("slim_block_fp8_weight", lib().slim_block_fp8_weight(_ptr(W), ld, DTYPES[W.dtype], n, k, cp, sp, _stream(W)))
     return codes, scales
 
 
@@ -688,7 +705,7 @@ def slim_block_fp8_tile(codes: torch.Tensor) -> torch.Tensor:
     """Row-major E4M3 codes [n][k] (uint8 or float8_e4m3fn, any row stride) -> uint8 in tiles, flat."""
     if codes.dtype not in (torch.uint8, _E4M3):
         raise ValueError("codes must be uint8 or float8_e4m3fn")
-    ld = _matrix(codes, codes, "codes")
+    ld = _rows(codes, "codes", codes.dtype, None, codes.get_device())
     n, k = codes.shape
     out = torch.empty(slim_block_fp8_weight_sizes(n, k)["codes"], dtype=torch.uint8, device=codes.device)
     _check("slim_block_fp8_tile", lib().slim_block_fp8_tile(_ptr(codes), ld, n, k, _ptr(out), _stream(codes)))
@@ -706,6 +723,12 @@ def slim_block_fp8_untile(codes: torch.Tensor, n: int, k: int) -> torch.Tensor:
 
 
 @dataclass
+class _LayerRef:
+    layer: object
+    device: int
+
+
+@dataclass
 class SlimBlockFp8Weight:
     """Device buffers of one layer of 8-bit weights (what `slim_block_fp8_layer` points at)."""
     n: int
@@ -714,8 +737,8 @@ class SlimBlockFp8Weight:
     scales: torch.Tensor           # float32 [ceil(n / 128)][ceil(k / 128)]
 
     def c_ref(self):
-        """Pointer argument for the product; the buffers are checked when it is made, once per layer and again
-        after any field is assigned."""
+        """What the product is given of the layer (`layer`: the pointer argument, `device`); the buffers are checked when it is made, once
+        per layer and again after any field is assigned."""
         ref = self.__dict__.get("_ref")
         if ref is None:
             size = slim_block_fp8_weight_sizes(self.n, self.k)
@@ -724,9 +747,9 @@ class SlimBlockFp8Weight:
             if self.codes.numel() != size["codes"] or self.scales.numel() * 4 != size["scales"] or self.scales.device != self.codes.device:
                 raise ValueError("codes and scales are not an n x k layer's on one device")
             cs = slim_block_fp8_layer(self.n, self.k, self.codes.data_ptr(), self.scales.data_ptr())
-            ref = (ctypes.byref(cs), cs)
+            ref = _LayerRef(ctypes.byref(cs), self.codes.get_device())          # (byref keeps the struct)
             self.__dict__["_ref"] = ref
-        return ref[0]
+        return ref
 
     def __setattr__(self, name, value):
         self.__dict__.pop("_ref", None)
@@ -753,29 +776,30 @@ def slim_block_fp8_gemm(layer: SlimBlockFp8Weight, codes: torch.Tensor, scales: 
     """Y [m][n] = inputs times weights^T on 8-bit inputs as slim_block_fp8_norm and slim_block_fp8_act return them, any m >= 1.
     Y: a float16, bfloat16 or float32 matrix (any row stride), or None for a new one of `dtype`."""
     ref = layer.c_ref()
-    kb = (layer.k + 127) // 128
-    if codes.dim() != 2 or codes.shape[1] != kb * 128 or codes.dtype not in (torch.uint8, _E4M3) or not codes.is_contiguous():
-        raise ValueError("codes must be contiguous uint8 [m][128 ceil(k / 128)]")
-    m, device = codes.shape[0], layer.codes.device
-    if scales.dtype != torch.float32 or scales.numel() != m * kb or not scales.is_contiguous():
-        raise ValueError("scales must be contiguous float32 [m][ceil(k / 128)]")
+    kb, n = (layer.k + 127) // 128, layer.n
+    m, cols = codes.shape
+    if cols != kb * 128:
+        raise ValueError("codes must be [m][128 ceil(k / 128)]")
+    device = ref.device
     if Y is None:
         if dtype not in DTYPES:
             raise ValueError("dtype is float16, bfloat16 or float32")
-        Y = torch.empty(m, layer.n, dtype=dtype, device=device)
-        ld = layer.n
+        Y = torch.empty(m, n, dtype=dtype, device=layer.codes.device)
     else:
-        if Y.dtype not in DTYPES:
+        dtype = Y.dtype
+        if dtype not in DTYPES:
             raise ValueError("Y must be float16, bfloat16 or float32")
-        ld = _matrix(Y, Y, "Y", (m, layer.n))
-    if codes.device != device or scales.device != device or Y.device != device:
-        raise ValueError("inputs, Y and the layer must be on one device")
+    ld = _rows(Y, "Y", dtype, (m, n), device)
     if workspace is None:
         workspace = alloc_block_fp8_workspace(layer, m)
-    elif workspace.device != device:
+    elif workspace.get_device() != device:
         raise ValueError("workspace must be on the layer's device")
-    status = lib().slim_block_fp8_gemm(ref, codes.data_ptr(), scales.data_ptr(), m, Y.data_ptr(), ld, DTYPES[Y.dtype], workspace.data_ptr(),
-                                       workspace.numel(), torch._C._cuda_getCurrentRawStream(device.index))
+    code_type = codes.dtype
+    if code_type is not torch.uint8 and code_type is not _E4M3:
+        raise ValueError("codes must be uint8 or float8_e4m3fn")
+    status = lib().slim_block_fp8_gemm(ref.layer, _whole(codes, "codes", code_type, m * cols, device),
+                                       _whole(scales, "scales", torch.float32, m * kb, device), m, Y.data_ptr(), ld, DTYPES[dtype],
+                                       workspace.data_ptr(), workspace.numel(), torch._C._cuda_getCurrentRawStream(device))
     if status != SLIM_OK:
         _check("slim_block_fp8_gemm", status)
     return Y
