@@ -224,13 +224,15 @@ __global__ __launch_bounds__(THREADS) void block_stream_kernel(BlockGemmArgs a)
 // the first of the 16.  A wavefront waits until no more of its loads are under way than the pieces of later blocks; that some of
 // those may be scales makes it wait longer, never shorter.
 // Results leave through LDS, so that a store instruction writes whole lines of a token's row.
+// KG = 2: two such groups of wavefronts share the tile, each with half of the blocks and buffers of its own, and their sums are added at the end: where
+// there are few tiles, twice the loads are under way, and a SIMD has two wavefronts with the larger share of the tile.
 template <int BM, int BN, int STAGES>
 struct TileLds {
     static constexpr int stage = (BM + BN) * kBlk, scales = STAGES * stage, chunk = BN * 64, bytes = scales + 2 * chunk;
 };
 
-template <int WR, int WT, int AF, int BF, int STAGES, bool EXACT, class T>
-__global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmArgs a)
+template <int KG, int WR, int WT, int AF, int BF, int STAGES, bool EXACT, class T>
+__global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockGemmArgs a)
 {
     typedef typename T::type E;
     constexpr int WAVES = WR * WT, BM = 16 * AF * WR, BN = 16 * BF * WT, TAIL = 2;
@@ -242,7 +244,8 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     static_assert(AF * 16 == 64 || (AF * 16) % kBlk == 0, "a wavefront's rows have one scale per block");
     static_assert(STAGES >= 2 && STAGES <= 8 && (int)(BM * BN * sizeof(E)) <= Lds::scales, "buffers");
     extern __shared__ __align__(16) uint8_t lds[];
-    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x & (kWave - 1);
+    const int group = wave / WAVES, w = wave % WAVES;
     const int wr = w % WR, wt = w / WR, j = lane & 15, q = lane >> 4;
     const int gx = a.tiles_o * a.tiles_t;
     const int qx = gx % kDies == 0 ? ((int)blockIdx.x % kDies) * (gx / kDies) + (int)blockIdx.x / kDies : (int)blockIdx.x;
@@ -255,7 +258,10 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     // rows past the layer's last block of 128 are zeros: any scale will do
     const int rb = min((o0 + wr * AF * 16) / kBlk, (a.n - 1) / kBlk);
     const float *ws = a.ws + (int64_t)rb * a.kb;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+    uint8_t *const own = lds + group * Lds::bytes;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)own;
+    // the group's blocks: count from `first` on (none where there is one block only), in as many turns as any group's
+    const int turns = (a.kb + KG - 1) / KG, first = group * turns, count = min(turns, a.kb - first);
 
     // this wavefront's shares of a block: a run of KiB of the weight tiles, and groups of eight tokens whose eight 16-byte pieces are put in another
     // order in each of eight rows, so that a fragment's reads find all banks
@@ -273,19 +279,19 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     auto fetch_scales = [&](int b) {
 #pragma unroll
         for (int i = 0; i < SL; ++i)
-            load_to_lds(sd, soff[i] + (uint32_t)b * 4u, 0u, lds0 + Lds::scales + (uint32_t)(b >> 4 & 1) * Lds::chunk + (uint32_t)(w * SL + i) * 1024u);
+            load_to_lds(sd, soff[i] + (uint32_t)(first + b) * 4u, 0u, lds0 + Lds::scales + (uint32_t)(b >> 4 & 1) * Lds::chunk + (uint32_t)(w * SL + i) * 1024u);
     };
-    // Unit `u` of this wavefront's share of block b.  Past the last block nothing is read (from a buffer of no length; zeros): the number of
+    // Unit `u` of this wavefront's share of the group's block b.  Past the last block nothing is read (from a buffer of no length; zeros): the number of
     // loads under way is the same everywhere.
     auto fetch_unit = [&](auto uc, int b, int buffer) {
         constexpr int u = decltype(uc)::value;
         const uint32_t base = lds0 + (uint32_t)buffer * Lds::stage;
         if constexpr (u < WU) {
-            const rsrc_t d = make_rsrc(wbase, b < a.kb ? (uint32_t)rows * kp : 0u);
-            load_run_to_lds<RUN, u * RUN * 1024>(d, woff[u], (uint32_t)b * kWTileBytes, base + (uint32_t)(w * WL) * 1024u);
+            const rsrc_t d = make_rsrc(wbase, b < count ? (uint32_t)rows * kp : 0u);
+            load_run_to_lds<RUN, u * RUN * 1024>(d, woff[u], (uint32_t)(first + b) * kWTileBytes, base + (uint32_t)(w * WL) * 1024u);
         } else {
-            const rsrc_t d = make_rsrc(xbase, b < a.kb ? (uint32_t)toks * kp : 0u);
-            load_run_to_lds<1, WB + (u - WU) * 1024>(d, xoff[u - WU], (uint32_t)b * kBlk, base + (uint32_t)(w * XL) * 1024u);
+            const rsrc_t d = make_rsrc(xbase, b < count ? (uint32_t)toks * kp : 0u);
+            load_run_to_lds<1, WB + (u - WU) * 1024>(d, xoff[u - WU], (uint32_t)(first + b) * kBlk, base + (uint32_t)(w * XL) * 1024u);
         }
     };
 
@@ -293,23 +299,25 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     // for all the loads under way, which it does not know of.
     float row_scales;
     auto fetch_row_scales = [&](int b) {
-        row_scales = ws[min(b + lane, a.kb - 1)];
+        row_scales = ws[min(first + b + lane, a.kb - 1)];
         asm volatile("" : "+v"(row_scales));
     };
     fetch_row_scales(0);
 
     const int xrow = (wt * BF * 16 + j) * kBlk, xp0 = (q ^ (j & 7)) * 16, xp1 = ((4 + q) ^ (j & 7)) * 16;
     auto load_x = [&](int buffer, int t) {
-        const uint8_t *row = lds + buffer * Lds::stage + WB + xrow + t * 16 * kBlk;
+        const uint8_t *row = own + buffer * Lds::stage + WB + xrow + t * 16 * kBlk;
         return Codes<EXACT>(*reinterpret_cast<const uint4_t *>(row + xp0), *reinterpret_cast<const uint4_t *>(row + xp1));
     };
     auto load_w = [&](int buffer, int i) {
-        const uint8_t *frag = lds + buffer * Lds::stage + (wr * AF + i) * 2048 + lane * 16;
+        const uint8_t *frag = own + buffer * Lds::stage + (wr * AF + i) * 2048 + lane * 16;
         return Codes<EXACT>(*reinterpret_cast<const uint4_t *>(frag), *reinterpret_cast<const uint4_t *>(frag + 1024));
     };
     auto load_scale = [&](int b, int t) {
-        return *reinterpret_cast<const float *>(lds + Lds::scales + (b >> 4 & 1) * Lds::chunk + ((wt * BF + t) * 16 + j) * 64 +
-                                                ((b >> 2 & 3) ^ (j >> 2)) * 16 + (b & 3) * 4);
+        const float v = *reinterpret_cast<const float *>(own + Lds::scales + (b >> 4 & 1) * Lds::chunk + ((wt * BF + t) * 16 + j) * 64 +
+                                                         ((b >> 2 & 3) ^ (j >> 2)) * 16 + (b & 3) * 4);
+        // (a group that has a block less than the other adds nothing in the last turn, whatever is there)
+        return KG == 1 || b < count ? v : 0.f;
     };
 
     float4_t acc[AF][BF];
@@ -324,7 +332,7 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     float s[BF], wsb;
     // The products of a block in order: fragment by fragment, the last TAIL token tile by token tile.  Each is added LAG products later, when the matrix
     // pipe has it ready.
-    constexpr int SLOTS = AF * BF, LAG = EXACT ? 1 : 3;
+    constexpr int SLOTS = AF * BF, LAG = EXACT ? 2 : 3;
     // A block's loads are asked for a few at a time between the products, EARLY units of them in the tail that follows the barrier and the others in the
     // next block: all at once they held the wavefronts up behind one another, 600 of 3170 cycles per block of 256 x 256.
     constexpr int SPREAD = SLOTS >= 2 * UNITS ? 2 : 1, EARLY = UNITS < (TAIL * BF + SPREAD - 1) / SPREAD ? UNITS : (TAIL * BF + SPREAD - 1) / SPREAD;
@@ -355,7 +363,7 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     }
     wv[0] = load_w(0, 0);
 
-    for (int b = 0, buffer = 0; b < a.kb; ++b) {
+    for (int b = 0, buffer = 0; b < turns; ++b) {
         const int after = buffer + 1 < STAGES ? buffer + 1 : 0, before = buffer > 0 ? buffer - 1 : STAGES - 1;
         static_for<MAIN * BF>([&](auto nc) {
             constexpr int n = decltype(nc)::value, i = row_of(n), t = token_of(n);
@@ -367,7 +375,7 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
                 fetch_unit(std::integral_constant<int, EARLY + n / SPREAD>{}, b + STAGES - 1, before);
             p[n % (LAG + 1)] = block_product(wv[place(i)], x[t]);
             if constexpr (n >= LAG) add(std::integral_constant<int, n - LAG>{});
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (!EXACT || n % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         });
         // The sums so far are made here: the compiler would put them off past the barrier, and spill the products.
 #pragma unroll
@@ -393,7 +401,7 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
             p[n % (LAG + 1)] = block_product(wv[place(i)], x[t]);
             if constexpr (i == AF - 1) x[t] = load_x(after, t);
             add(std::integral_constant<int, n - LAG>{});
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (!EXACT || n % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         });
         static_for<LAG>([&](auto nc) { add(std::integral_constant<int, SLOTS - LAG + decltype(nc)::value>{}); });
 #pragma unroll
@@ -406,6 +414,20 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
+    if constexpr (KG > 1) {
+        float4_t *part = reinterpret_cast<float4_t *>(lds);          // [SLOTS][WAVES][64]
+        if (group == 1) {
+#pragma unroll
+            for (int n = 0; n < SLOTS; ++n) part[(n * WAVES + w) * kWave + lane] = acc[n / BF][n % BF];
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int n = 0; n < SLOTS; ++n) acc[n / BF][n % BF] += part[(n * WAVES + w) * kWave + lane];
+        }
+        __syncthreads();
+    }
+    if (group == 0)
 #pragma unroll
     for (int t = 0; t < BF; ++t) {
         const int tok = (wt * BF + t) * 16 + j;
@@ -422,7 +444,7 @@ __global__ __launch_bounds__(WR *WT *kWave, 2) void block_tile_kernel(BlockGemmA
             }
     }
     __syncthreads();
-    for (int i = (int)threadIdx.x; i < toks * PER_ROW; i += WAVES * kWave) {
+    for (int i = (int)threadIdx.x; i < toks * PER_ROW; i += KG * WAVES * kWave) {
         const int tok = i / PER_ROW, c = i % PER_ROW, o = o0 + c * PIECE;
         if (o < a.n) {
             typedef E vec __attribute__((ext_vector_type(PIECE)));
@@ -472,31 +494,41 @@ static void launch_stream_of(const BlockGemmArgs &a, hipStream_t st)
     launch_stream<1, TB, T>(a, fragments < 256 ? 8 : 4, st);
 }
 
-template <int WR, int WT, int AF, int BF, int STAGES, bool EXACT, class T>
+template <int KG, int WR, int WT, int AF, int BF, int STAGES, bool EXACT, class T>
 static int launch_tile(BlockGemmArgs a, hipStream_t st)
 {
     constexpr int BM = 16 * AF * WR, BN = 16 * BF * WT;
-    constexpr size_t LDS = TileLds<BM, BN, STAGES>::bytes;
+    constexpr size_t LDS = (size_t)KG * TileLds<BM, BN, STAGES>::bytes;
+    static_assert(KG <= 2 && LDS <= 160 * 1024 && (KG == 1 || (size_t)BM * BN * 4 <= LDS), "LDS");
     a.tiles_o = (int)(((int64_t)a.n + BM - 1) / BM);
     a.tiles_t = (int)(((int64_t)a.m + BN - 1) / BN);
     const int64_t tiles = (int64_t)a.tiles_o * a.tiles_t;
-    if (tiles * (WR * WT * kWave) > UINT32_MAX) return SLIM_ERR_SHAPE;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(block_tile_kernel<WR, WT, AF, BF, STAGES, EXACT, T>), dim3((unsigned)tiles), dim3(WR * WT * kWave), LDS,
+    if (tiles * (KG * WR * WT * kWave) > UINT32_MAX) return SLIM_ERR_SHAPE;
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(block_tile_kernel<KG, WR, WT, AF, BF, STAGES, EXACT, T>), dim3((unsigned)tiles), dim3(KG * WR * WT * kWave), LDS,
                        st, a);
     return SLIM_OK;
 }
 
 // Tiles of block_tile_kernel: rows, tokens, workgroups per compute unit (by LDS), and the time per block of 128 inputs with every compute unit
-// at work and with at most half of them (less power, less traffic).  The times (us) are those of single rounds on 4096 to
-// 11008 inputs; a call takes rounds * (blocks * time + 3) or so, and the tile with the least of that is taken.  The smaller tiles
-// are bound by the instructions a wavefront issues per block (its 32 additions per 8 products first of all), 256 x 256 by power.
+// at work and with at most half of them (less power, less traffic).  The times (us) are those of one to three rounds on 128 to
+// 4096 tokens, 4096 to 28672 rows and 4096 to 11008 inputs; a call takes rounds * (blocks * time + 3) or so, and the tile with the least of that
+// is taken.  us so, with the tiles in their order (the one taken in brackets):
+//   128 tokens, 4096 x 4096      44  29  19  15  12.0 [10.4]
+//   256 tokens, 5120 x 5120      55  35  23 [18] 18  23
+//   333 tokens, 10007 x 4100     48  31 [24] 31  32  40
+//   512 tokens, 4096 x 11008    110  68  43 [35] 39  42
+//   1000 tokens, 8192 x 8192     85 [67] 82 108 113
+//   1024 tokens, 11008 x 4096   [49] 62  64  88  82
+// The smaller tiles are bound by the instructions a wavefront issues per block (its 32 additions per 8 products first of all), 256 x 256 by power.
 struct TileShape {
     int rows, toks, per_cu;
     float full, half;
 };
-constexpr TileShape kTiles[] = {{256, 256, 1, 1.7f, 1.3f}, {256, 128, 1, 1.0f, 0.8f}, {128, 128, 1, 0.62f, 0.5f},
-                                {64, 128, 1, 0.40f, 0.38f}, {64, 64, 2, 0.45f, 0.33f}};
-constexpr TileShape kExactTiles[] = {{128, 128, 2, 1.6f, 1.2f}, {128, 128, 1, 1.17f, 1.1f}, {64, 64, 2, 0.76f, 0.53f}};
+constexpr TileShape kTiles[] = {{256, 256, 1, 1.7f, 1.3f},   {256, 128, 1, 1.0f, 0.8f},  {128, 128, 1, 0.62f, 0.5f},
+                                {64, 128, 1, 0.40f, 0.38f}, {64, 64, 2, 0.45f, 0.33f}, {64, 64, 1, 0.24f, 0.24f}};
+// (with results in fp32: 128 x 128, the same by two groups, 64 x 128 and 64 x 64 by two groups; 333 tokens on 10007 x 4100: 42, [38], 49, 65;
+// 1024 tokens on 11008 x 4096: [90], 98, 133, 167; 128 tokens on 4096 x 4096: 39, 32, 23, [16])
+constexpr TileShape kExactTiles[] = {{128, 128, 2, 1.31f, 1.1f}, {128, 128, 1, 0.97f, 0.92f}, {64, 128, 1, 0.64f, 0.64f}, {64, 64, 1, 0.42f, 0.42f}};
 
 static int plan_tile(const BlockGemmArgs &a, bool exact)
 {
@@ -532,17 +564,19 @@ static int launch_block_gemm(const BlockGemmArgs &a, hipStream_t st)
     const int shape = plan_tile(a, EXACT);
     if constexpr (EXACT) {
         switch (shape) {
-        case 0: return launch_tile<2, 2, 4, 4, 2, true, T>(a, st);
-        case 1: return launch_tile<2, 4, 4, 2, 4, true, T>(a, st);
-        default: return launch_tile<1, 4, 4, 1, 4, true, T>(a, st);
+        case 0: return launch_tile<1, 2, 2, 4, 4, 2, true, T>(a, st);
+        case 1: return launch_tile<2, 2, 2, 4, 4, 2, true, T>(a, st);
+        case 2: return launch_tile<2, 1, 4, 4, 2, 2, true, T>(a, st);
+        default: return launch_tile<2, 1, 4, 4, 1, 4, true, T>(a, st);
         }
     } else {
         switch (shape) {
-        case 0: return launch_tile<2, 4, 8, 4, 2, false, T>(a, st);
-        case 1: return launch_tile<4, 2, 4, 4, 3, false, T>(a, st);
-        case 2: return launch_tile<2, 4, 4, 2, 4, false, T>(a, st);
-        case 3: return launch_tile<1, 4, 4, 2, 4, false, T>(a, st);
-        default: return launch_tile<1, 4, 4, 1, 4, false, T>(a, st);
+        case 0: return launch_tile<1, 2, 4, 8, 4, 2, false, T>(a, st);
+        case 1: return launch_tile<1, 4, 2, 4, 4, 3, false, T>(a, st);
+        case 2: return launch_tile<1, 2, 4, 4, 2, 4, false, T>(a, st);
+        case 3: return launch_tile<1, 1, 4, 4, 2, 4, false, T>(a, st);
+        case 4: return launch_tile<1, 1, 4, 4, 1, 4, false, T>(a, st);
+        default: return launch_tile<2, 1, 4, 4, 1, 4, false, T>(a, st);
         }
     }
 }
