@@ -43,6 +43,16 @@ struct NormArgs {
     bool gain32;
 };
 
+// A piece of 8 elements of a row as they are stored, zeros from element `len` on.
+template <class T>
+__device__ __forceinline__ typename Piece<T, 8>::vec raw_piece(const typename T::type *row, int at, int len)
+{
+    if (at + 8 <= len) return Piece<T, 8>::load(row + at);
+    typename Piece<T, 8>::vec v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = at + e < len ? row[at + e] : (typename T::type)0.f;
+    return v;
+}
 // h of one piece of 8.
 template <class T>
 __device__ __forceinline__ void norm_load(const NormArgs &a, int64_t row, int at, float (&h)[8])
@@ -77,6 +87,7 @@ template <class T, int NV, bool LONG>
 __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a)
 {
     typedef typename T::type E;
+    typedef typename Piece<T, 8>::vec V;
     __shared__ float red[2][16];
     const int kp = a.kb * kBlk, step = 8 * (int)blockDim.x, waves = (int)blockDim.x / kWave, first = 8 * (int)threadIdx.x;
     int turn = 0;
@@ -111,10 +122,25 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a)
 
     if constexpr (!LONG) {
         for (int64_t row = blockIdx.x; row < a.m; row += gridDim.x) {
+            // all loads first, as they are stored
+            V x[NV], r[NV];
+#pragma unroll
+            for (int p = 0; p < NV; ++p) {
+                const int at = first + p * step;
+                if (at < kp) {
+                    x[p] = raw_piece<T>(static_cast<const E *>(a.X) + row * a.x_ld, at, a.k);
+                    if (a.res) r[p] = raw_piece<T>(static_cast<const E *>(a.res) + row * a.res_ld, at, a.k);
+                }
+            }
             float z[NV][8], sc[NV], sum = 0.f;
 #pragma unroll
-            for (int p = 0; p < NV; ++p)
-                if (first + p * step < kp) norm_load<T>(a, row, first + p * step, z[p]);
+            for (int p = 0; p < NV; ++p) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    z[p][e] = (float)x[p][e];
+                    if (a.res) z[p][e] += (float)r[p][e];
+                }
+            }
 #pragma unroll
             for (int p = 0; p < NV; ++p) {
                 const int at = first + p * step;
