@@ -582,7 +582,26 @@ ACTS = {"none": 0, "silu": 1}
 _E4M3 = torch.float8_e4m3fn
 
 
-# A call on one token is a few microseconds and every look at a tensor a twentieth of one: each argument is looked at once.
+_call = None
+
+
+def _calls():
+    """The block operators' calls with their arguments looked at in C (csrc/slim_args.c), made ready once."""
+    global _call
+    if _call is None:
+        L = lib()
+        try:
+            from paper_2410_09615_amd import _slim_args
+        except ImportError as e:
+            raise RuntimeError("the _slim_args extension is missing: build it with `python -m paper_2410_09615_amd.build` "
+                               "(there is no fallback path)") from e
+        entry = lambda f: ctypes.cast(f, ctypes.c_void_p).value
+        _slim_args.init((torch.float16, torch.bfloat16, torch.float32, torch.uint8, _E4M3), torch._C._cuda_getCurrentRawStream,
+                        entry(L.slim_block_fp8_norm), entry(L.slim_block_fp8_act), entry(L.slim_block_fp8_gemm))
+        _call = _slim_args
+    return _call
+
+
 def _rows(t: torch.Tensor, name: str, dtype, shape, device: int) -> int:
     """t's row stride; t is a matrix of `shape` (None: any) and `dtype` on `device`, whose rows have no gaps, whatever lies between them."""
     at = t.get_device()
@@ -620,37 +639,12 @@ def slim_block_fp8_norm(X: torch.Tensor, gain: torch.Tensor | None = None, eps: 
     """h = X + residual, y = h gain / sqrt(mean(h^2) + eps) -> (codes uint8 [m][128 kb], scales fp32 [m][kb], H, Y): y in 8 bits with a
     scale per 128 inputs.  H, Y: True for a new matrix of X's type, or one to write (X or residual itself, for in place);
     None (returned as such): not wanted.  X, residual, H, Y fp16 or bf16 with any row stride; gain of X's type or fp32."""
-    device, dtype, shape = X.get_device(), X.dtype, X.shape
-    if dtype is not torch.float16 and dtype is not torch.bfloat16:
-        raise ValueError("X must be float16 or bfloat16")
-    x_ld = _rows(X, "X", dtype, None, device)
-    m, k = shape
-    kb = (k + 127) // 128
-    r_ld = h_ld = y_ld = 0
-    rp = hp = yp = gp = None
-    xt = gt = DTYPES[dtype]
-    if residual is not None:
-        r_ld, rp = _rows(residual, "residual", dtype, shape, device), residual.data_ptr()
-    if gain is not None:
-        gd = gain.dtype
-        if gd is torch.float32:
-            gt = 2
-        elif gd is not dtype:
-            raise ValueError("gain must be of X's type or float32")
-        gp = _whole(gain, "gain", gd, k, device)
-    if H is not None:
-        if H is True:
-            H = torch.empty(m, k, dtype=dtype, device=X.device)
-        h_ld, hp = _rows(H, "H", dtype, shape, device), H.data_ptr()
-    if Y is not None:
-        if Y is True:
-            Y = torch.empty(m, k, dtype=dtype, device=X.device)
-        y_ld, yp = _rows(Y, "Y", dtype, shape, device), Y.data_ptr()
-    if codes is None or scales is None:
+    if codes is None or scales is None or H is True or Y is True:
+        m, k = X.shape
         codes, scales = _code_buffers(m, k, codes, scales, X.device)
-    status = lib().slim_block_fp8_norm(X.data_ptr(), x_ld, rp, r_ld, gp, gt, xt, m, k, eps, hp, h_ld, yp, y_ld,
-                                       _whole(codes, "codes", torch.uint8, m * kb * 128, device),
-                                       _whole(scales, "scales", torch.float32, m * kb, device), torch._C._cuda_getCurrentRawStream(device))
+        H = torch.empty_like(X, memory_format=torch.contiguous_format) if H is True else H
+        Y = torch.empty_like(X, memory_format=torch.contiguous_format) if Y is True else Y
+    status = (_call or _calls()).norm(X, gain, eps, residual, codes, scales, H, Y)
     if status != SLIM_OK:
         _check("slim_block_fp8_norm", status)
     return codes, scales, H, Y
@@ -659,20 +653,12 @@ def slim_block_fp8_norm(X: torch.Tensor, gain: torch.Tensor | None = None, eps: 
 def slim_block_fp8_act(G: torch.Tensor, U: torch.Tensor | None = None, act: str = "silu", codes=None, scales=None):
     """act(G) * U ("silu" or "none"; U None: act(G)) -> (codes uint8 [m][128 kb], scales fp32 [m][kb]).  G, U fp16 or bf16 [m][k] with any
     row stride: the halves of one product's output, for one.  act="none" without U quantizes an input as it is."""
-    device, dtype, shape = G.get_device(), G.dtype, G.shape
-    if dtype is not torch.float16 and dtype is not torch.bfloat16:
-        raise ValueError("G must be float16 or bfloat16")
-    if act not in ACTS:
+    kind = ACTS.get(act)
+    if kind is None:
         raise ValueError("act is 'silu' or 'none'")
-    g_ld = _rows(G, "G", dtype, None, device)
-    m, k = shape
-    kb = (k + 127) // 128
-    u_ld, up = (0, None) if U is None else (_rows(U, "U", dtype, shape, device), U.data_ptr())
     if codes is None or scales is None:
-        codes, scales = _code_buffers(m, k, codes, scales, G.device)
-    status = lib().slim_block_fp8_act(G.data_ptr(), g_ld, up, u_ld, ACTS[act], DTYPES[dtype], m, k,
-                                      _whole(codes, "codes", torch.uint8, m * kb * 128, device),
-                                      _whole(scales, "scales", torch.float32, m * kb, device), torch._C._cuda_getCurrentRawStream(device))
+        codes, scales = _code_buffers(*G.shape, codes, scales, G.device)
+    status = (_call or _calls()).act(G, U, kind, codes, scales)
     if status != SLIM_OK:
         _check("slim_block_fp8_act", status)
     return codes, scales
@@ -724,7 +710,8 @@ def slim_block_fp8_untile(codes: torch.Tensor, n: int, k: int) -> torch.Tensor:
 
 @dataclass
 class _LayerRef:
-    layer: object
+    layer: slim_block_fp8_layer
+    address: int
     device: int
 
 
@@ -737,8 +724,8 @@ class SlimBlockFp8Weight:
     scales: torch.Tensor           # float32 [ceil(n / 128)][ceil(k / 128)]
 
     def c_ref(self):
-        """What the product is given of the layer (`layer`: the pointer argument, `device`); the buffers are checked when it is made, once
-        per layer and again after any field is assigned."""
+        """What the product is given of the layer; the buffers are checked when it is made, once per layer and again after any field is
+        assigned."""
         ref = self.__dict__.get("_ref")
         if ref is None:
             size = slim_block_fp8_weight_sizes(self.n, self.k)
@@ -747,7 +734,7 @@ class SlimBlockFp8Weight:
             if self.codes.numel() != size["codes"] or self.scales.numel() * 4 != size["scales"] or self.scales.device != self.codes.device:
                 raise ValueError("codes and scales are not an n x k layer's on one device")
             cs = slim_block_fp8_layer(self.n, self.k, self.codes.data_ptr(), self.scales.data_ptr())
-            ref = _LayerRef(ctypes.byref(cs), self.codes.get_device())          # (byref keeps the struct)
+            ref = _LayerRef(cs, ctypes.addressof(cs), self.codes.get_device())
             self.__dict__["_ref"] = ref
         return ref
 
@@ -776,30 +763,13 @@ def slim_block_fp8_gemm(layer: SlimBlockFp8Weight, codes: torch.Tensor, scales: 
     """Y [m][n] = inputs times weights^T on 8-bit inputs as slim_block_fp8_norm and slim_block_fp8_act return them, any m >= 1.
     Y: a float16, bfloat16 or float32 matrix (any row stride), or None for a new one of `dtype`."""
     ref = layer.c_ref()
-    kb, n = (layer.k + 127) // 128, layer.n
-    m, cols = codes.shape
-    if cols != kb * 128:
-        raise ValueError("codes must be [m][128 ceil(k / 128)]")
-    device = ref.device
     if Y is None:
         if dtype not in DTYPES:
             raise ValueError("dtype is float16, bfloat16 or float32")
-        Y = torch.empty(m, n, dtype=dtype, device=layer.codes.device)
-    else:
-        dtype = Y.dtype
-        if dtype not in DTYPES:
-            raise ValueError("Y must be float16, bfloat16 or float32")
-    ld = _rows(Y, "Y", dtype, (m, n), device)
+        Y = torch.empty(codes.shape[0], layer.n, dtype=dtype, device=layer.codes.device)
     if workspace is None:
-        workspace = alloc_block_fp8_workspace(layer, m)
-    elif workspace.get_device() != device:
-        raise ValueError("workspace must be on the layer's device")
-    code_type = codes.dtype
-    if code_type is not torch.uint8 and code_type is not _E4M3:
-        raise ValueError("codes must be uint8 or float8_e4m3fn")
-    status = lib().slim_block_fp8_gemm(ref.layer, _whole(codes, "codes", code_type, m * cols, device),
-                                       _whole(scales, "scales", torch.float32, m * kb, device), m, Y.data_ptr(), ld, DTYPES[dtype],
-                                       workspace.data_ptr(), workspace.numel(), torch._C._cuda_getCurrentRawStream(device))
+        workspace = alloc_block_fp8_workspace(layer, codes.shape[0])
+    status = (_call or _calls()).gemm(ref.address, ref.device, codes, scales, Y, workspace)
     if status != SLIM_OK:
         _check("slim_block_fp8_gemm", status)
     return Y

@@ -1,4 +1,4 @@
-"""Build libslim.so (the HIP kernels + C-ABI) in-tree with hipcc for gfx950."""
+"""Build libslim.so (the HIP kernels + C-ABI) in-tree with hipcc for gfx950, and the binding's extension with the C compiler."""
 from __future__ import annotations
 
 import glob
@@ -6,12 +6,14 @@ import os
 import re
 import subprocess
 import sys
+import sysconfig
 import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libslim.so")
+ARGS = os.path.join(PKG, "_slim_args" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -109,10 +111,18 @@ def lane_reads_too_early(asm_text: str) -> dict:
     return out
 
 
+def build_args() -> str:
+    """Compile the binding's argument marshalling (csrc/slim_args.c)."""
+    subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-Wextra", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I",
+                    os.path.join(ROOT, "include"), "-o", ARGS, os.path.join(CSRC, "slim_args.c")], check=True)
+    return ARGS
+
+
 def build(verbose: bool = False) -> str:
     """Compile the library; the device assembly (a by-product of the same compilation) is checked for reads of other lanes' registers
     that come too early and, of the fixed-accumulator kernels, for accumulation registers used by the compiler."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    build_args()
     cmd = [hipcc, *HIPCC_FLAGS, "-save-temps", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", LIB, *sources()]
     if verbose:
         print(" ".join(cmd), flush=True)

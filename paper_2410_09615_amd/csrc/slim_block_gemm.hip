@@ -373,8 +373,8 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
             }
             if constexpr (n % SPREAD == 0 && EARLY + n / SPREAD < UNITS)
                 fetch_unit(std::integral_constant<int, EARLY + n / SPREAD>{}, b + STAGES - 1, before);
-            p[n % (LAG + 1)] = block_product(wv[place(i)], x[t]);
             if constexpr (n >= LAG) add(std::integral_constant<int, n - LAG>{});
+            p[n % (LAG + 1)] = block_product(wv[place(i)], x[t]);
             if constexpr (!EXACT || n % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         });
         // The sums so far are made here: the compiler would put them off past the barrier, and spill the products.

@@ -3,6 +3,7 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import block_fp8 as O
 from paper_2410_09615_amd import binding as B
@@ -112,3 +113,19 @@ def test_oracle_values_and_codes_agree(seed):
     v = np.random.default_rng(seed).normal(0, 100, 1000)
     r = O.fp8_round(v, "e4m3")
     assert np.array_equal(O.values(O.fp8_encode(r, "e4m3")), r)
+
+
+def test_binding_refuses_what_is_not_on_a_device():
+    """The arguments are looked at in C, type and device first: nothing here reaches the library."""
+    X = torch.zeros(4, 256, dtype=torch.float16)
+    codes, scales = torch.zeros(4, 256, dtype=torch.uint8), torch.zeros(4, 2)
+    layer = B.SlimBlockFp8Weight(64, 256, torch.zeros(64 * 256, dtype=torch.uint8), torch.zeros(1, 2))
+    for bad in (lambda: B.slim_block_fp8_norm(X), lambda: B.slim_block_fp8_norm(X.double(), codes=codes, scales=scales),
+                lambda: B.slim_block_fp8_norm(X, codes=codes, scales=scales, H=X, Y=X), lambda: B.slim_block_fp8_act(X, codes=codes, scales=scales),
+                lambda: B.slim_block_fp8_act(X, act="gelu"), lambda: B.slim_block_fp8_weight(X), lambda: B.slim_block_fp8_tile(codes),
+                lambda: B.slim_block_fp8_gemm(layer, codes, scales, workspace=codes)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: B.slim_block_fp8_norm(None, codes=codes, scales=scales), lambda: B.slim_block_fp8_act(3, codes=codes, scales=scales)):
+        with pytest.raises((AttributeError, TypeError)):
+            bad()
