@@ -307,11 +307,11 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
     const int xrow = (wt * BF * 16 + j) * kBlk, xp0 = (q ^ (j & 7)) * 16, xp1 = ((4 + q) ^ (j & 7)) * 16;
     auto load_x = [&](int buffer, int t) {
         const uint8_t *row = own + buffer * Lds::stage + WB + xrow + t * 16 * kBlk;
-        return Codes<EXACT>(*reinterpret_cast<const uint4_t *>(row + xp0), *reinterpret_cast<const uint4_t *>(row + xp1));
+        return Codes<false>(*reinterpret_cast<const uint4_t *>(row + xp0), *reinterpret_cast<const uint4_t *>(row + xp1));
     };
     auto load_w = [&](int buffer, int i) {
         const uint8_t *frag = own + buffer * Lds::stage + (wr * AF + i) * 2048 + lane * 16;
-        return Codes<EXACT>(*reinterpret_cast<const uint4_t *>(frag), *reinterpret_cast<const uint4_t *>(frag + 1024));
+        return Codes<false>(*reinterpret_cast<const uint4_t *>(frag), *reinterpret_cast<const uint4_t *>(frag + 1024));
     };
     auto load_scale = [&](int b, int t) {
         const float v = *reinterpret_cast<const float *>(own + Lds::scales + (b >> 4 & 1) * Lds::chunk + ((wt * BF + t) * 16 + j) * 64 +
@@ -328,8 +328,16 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
     // Row fragments in registers: two in turn, and the last TAIL, which are all read before the barrier, in their own.
     constexpr int MAIN = AF - TAIL, WBUF = TAIL > 1 ? 2 + TAIL : 2;
     auto place = [](int i) { return i < MAIN || TAIL == 1 ? i % 2 : 2 + i - MAIN; };
-    Codes<EXACT> x[BF], wv[WBUF];
+    Codes<false> x[BF], wv[WBUF];
     float s[BF], wsb;
+    // EXACT: what is being multiplied as fp16 numbers, made of the codes when the products begin (by then they are there)
+    Codes<true> xh[EXACT ? BF : 1], wh[EXACT ? TAIL : 1];
+    auto product = [&](int i, int t) {
+        if constexpr (EXACT)
+            return block_product(wh[i < MAIN ? 0 : i - MAIN], xh[t]);
+        else
+            return block_product(wv[place(i)], x[t]);
+    };
     // The products of a block in order: fragment by fragment, the last TAIL token tile by token tile.  Each is added LAG products later, when the matrix
     // pipe has it ready.
     constexpr int SLOTS = AF * BF, LAG = EXACT ? 2 : 3;
@@ -370,11 +378,13 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
             if constexpr (t == 0) {
                 if constexpr (i + 1 < MAIN || TAIL == 1) wv[place(i + 1)] = load_w(buffer, i + 1);
                 if constexpr (TAIL > 1 && i >= MAIN - TAIL) wv[place(i + TAIL)] = load_w(buffer, i + TAIL);
+                if constexpr (EXACT) wh[0] = Codes<true>(wv[place(i)].h[0], wv[place(i)].h[1]);
             }
+            if constexpr (EXACT && i == 0) xh[t] = Codes<true>(x[t].h[0], x[t].h[1]);
             if constexpr (n % SPREAD == 0 && EARLY + n / SPREAD < UNITS)
                 fetch_unit(std::integral_constant<int, EARLY + n / SPREAD>{}, b + STAGES - 1, before);
             if constexpr (n >= LAG) add(std::integral_constant<int, n - LAG>{});
-            p[n % (LAG + 1)] = block_product(wv[place(i)], x[t]);
+            p[n % (LAG + 1)] = product(i, t);
             if constexpr (!EXACT || n % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         });
         // The sums so far are made here: the compiler would put them off past the barrier, and spill the products.
@@ -393,12 +403,16 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
 #pragma unroll
         for (int t = 0; t < BF; ++t) sn[t] = load_scale(b + 1, t);
         wv[0] = load_w(after, 0);
+        if constexpr (EXACT) {
+#pragma unroll
+            for (int i = 0; i < TAIL; ++i) wh[i] = Codes<true>(wv[place(MAIN + i)].h[0], wv[place(MAIN + i)].h[1]);
+        }
         __builtin_amdgcn_sched_barrier(0);
         static_for<TAIL * BF>([&](auto nc) {
             constexpr int n = MAIN * BF + decltype(nc)::value, i = row_of(n), t = token_of(n);
             if constexpr ((n - MAIN * BF) % SPREAD == 0 && (n - MAIN * BF) / SPREAD < EARLY)
                 fetch_unit(std::integral_constant<int, (n - MAIN * BF) / SPREAD>{}, b + STAGES, buffer);
-            p[n % (LAG + 1)] = block_product(wv[place(i)], x[t]);
+            p[n % (LAG + 1)] = product(i, t);
             if constexpr (i == AF - 1) x[t] = load_x(after, t);
             add(std::integral_constant<int, n - LAG>{});
             if constexpr (!EXACT || n % 2 == 1) __builtin_amdgcn_sched_barrier(0);
