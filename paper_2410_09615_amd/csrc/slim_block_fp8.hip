@@ -81,8 +81,10 @@ __device__ __forceinline__ void gain_piece(const NormArgs &a, int at, float (&g)
 
 // A row per workgroup, NV pieces of 8 values per lane, held in registers from the one read to the last write (more rows than
 // workgroups fit into a grid are walked).  LONG: rows that do not fit so are read twice, the sum first.
-// Bound by memory: 4096 x 8192 in fp16 with a residual moves 236 MB in 48 us, 4.9 TB/s, the rate of a large copy (5.0).  Workgroups that
-// stay and walk the rows with the next row's loads under way, 2 to 32 of them per compute unit, took 48 to 57 us.
+// Bound by memory: 4096 x 8192 in fp16 with a residual moves 236 MB in 49 us, 4.8 TB/s (a large copy: 5.15); 1777 x 5003 in bf16, whose rows begin
+// at odd elements, 80 MB in 19.7 us (13 % of it for that).  One row of 8192 takes 3.7 us: the launch, one read, the sum across
+// wavefronts, one write.  Workgroups that stay and walk the rows with the next row's loads under way, 2 to 32 of them per compute unit, took 48 to 57 us.
+// 1 / sqrt and not the approximation: once per row.
 template <class T, int NV, bool LONG>
 __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a)
 {
@@ -191,7 +193,9 @@ struct ActArgs {
     int k, kb;
 };
 
-// 16 lanes per block.  A lane takes one piece per round; nothing is shared between blocks.
+// 16 lanes per block.  A lane takes one piece per round; nothing is shared between blocks, so the largest of a block is found in registers and the
+// values are read once.  Bound by memory: 2048 x 11008 in bf16, gated, moves 114 MB in 23 us, 5.0 TB/s (a large copy: 5.15); 16 x 13824 takes
+// 3.0 us, a launch and one dependent access.  exp and the division in 32 bits; the result is rounded once, to its code.
 template <class T, bool SILU>
 __global__ __launch_bounds__(256) void act_kernel(ActArgs a)
 {
@@ -225,8 +229,9 @@ __device__ __forceinline__ uint32_t wtile_lds(uint32_t place)
     return ((piece ^ ((piece >> 4) & 7u)) << 4) | (place & 15u);
 }
 
-// One workgroup per 128 x 128 weights: in registers while their largest is found, then through LDS into the order of the tiles.
-// VEC values of 16 bytes per lane and load.
+// One workgroup per 128 x 128 weights: in registers while their largest is found (so they are read once), then through LDS into the order of the tiles.
+// VEC values of 16 bytes per lane and load.  Bound by memory: 28672 x 8192 in bf16 moves 705 MB in 129 us, 5.5 TB/s (a large copy: 5.15, half of it
+// writes; here a third); 4096 x 4096 in fp32 84 MB in 14.5 us.
 template <class T>
 __global__ __launch_bounds__(256) void weight_kernel(const typename T::type *W, int64_t ld, int n, int k, int kb, uint8_t *codes, float *scales)
 {
@@ -278,7 +283,7 @@ __global__ __launch_bounds__(256) void weight_kernel(const typename T::type *W, 
     }
 }
 
-// Row-major codes to tiles (TILE), or back: one lane per piece of 16 inputs of a row of the padded matrix.
+// Row-major codes to tiles (TILE), or back: one lane per piece of 16 inputs of a row of the padded matrix.  Once per layer, so no more than right.
 template <bool TILE>
 __global__ __launch_bounds__(256) void retile_kernel(const uint8_t *in, int64_t ld, int n, int k, int kb, int64_t pieces, uint8_t *out)
 {

@@ -109,6 +109,9 @@ __device__ __forceinline__ void load_run_to_lds(rsrc_t r, uint32_t lane_off, uin
 // pipeline of its own: D blocks' operands of its share are under way to its own part of LDS (loads that write LDS; the tokens' as eight rows of
 // 128 bytes per load, in the order of block_tile_kernel's: as a fragment needs them, 16 rows of 64, they take more than twice the time).
 // The S partial results meet in LDS and are added in order.
+// Bound by memory where the layer is large: 28672 x 8192 at 16 tokens 44 us, 5.3 TB/s, and 42 to 44 with the products left out.  Layers that fit the
+// last-level cache are bound by what a wavefront issues, conversions to fp16 first: 5120 x 5120 at 48 tokens 9.7 us on 160 of 256 compute units (more
+// workgroups of fewer fragments convert the tokens more often, the times are at launch_stream_of); 4096 x 4096 at one token 5.3 us, of which a launch is 3.
 template <int FR, int TB>
 struct StreamLds {
     static constexpr int stage = (FR + TB) * 2048, scales = 2048;         // per wavefront: of a block; of twice four blocks
@@ -224,6 +227,10 @@ __global__ __launch_bounds__(THREADS) void block_stream_kernel(BlockGemmArgs a)
 // the first of the 16.  A wavefront waits until no more of its loads are under way than the pieces of later blocks; that some of
 // those may be scales makes it wait longer, never shorter.
 // Results leave through LDS, so that a store instruction writes whole lines of a token's row.
+// 28672 x 8192 at 4096 tokens takes 760 to 782 us from card to card, 2.53 PFLOP/s (671 us for the library's product with one scale in all): power holds the clock at 1.65 GHz,
+// the matrix pipes are busy 68 % of it; without the scaled additions, 4 of a lane's instructions per product, it would be 661, without
+// loads 595.  10007 x 4100 at 333 tokens in fp32 (EXACT) takes 35.3 us at 2.4 GHz, matrix pipes 32 % busy: chains of four products and the conversions
+// between them; chains of two products issued in turn by hand were no faster (35.4).
 // KG = 2: two such groups of wavefronts share the tile, each with half of the blocks and buffers of its own, and their sums are added at the end: where
 // there are few tiles, twice the loads are under way, and a SIMD has two wavefronts with the larger share of the tile.
 template <int BM, int BN, int STAGES>
@@ -527,12 +534,13 @@ static int launch_tile(BlockGemmArgs a, hipStream_t st)
 // at work and with at most half of them (less power, less traffic).  The times (us) are those of one to three rounds on 128 to
 // 4096 tokens, 4096 to 28672 rows and 4096 to 11008 inputs; a call takes rounds * (blocks * time + 3) or so, and the tile with the least of that
 // is taken.  us so, with the tiles in their order (the one taken in brackets):
-//   128 tokens, 4096 x 4096      44  29  19  15  12.0 [10.4]
-//   256 tokens, 5120 x 5120      55  35  23 [18] 18  23
-//   333 tokens, 10007 x 4100     48  31 [24] 31  32  40
-//   512 tokens, 4096 x 11008    110  68  43 [35] 39  42
-//   1000 tokens, 8192 x 8192     85 [67] 82 108 113
-//   1024 tokens, 11008 x 4096   [49] 62  64  88  82
+//   128 tokens, 4096 x 4096      41  27  19  15  12.0 [10.4]
+//   256 tokens, 5120 x 5120      52  33  23 [18] 18  23
+//   333 tokens, 10007 x 4100     46  29 [22] 31  31  39
+//   512 tokens, 4096 x 11008    104  64  43 [35] 38  41
+//   700 tokens, 4096 x 4096      43  28 [19] 29  25  28
+//   1000 tokens, 8192 x 8192     80 [63] 77 105 108 125
+//   1024 tokens, 11008 x 4096   [46] 60  60  83  78  97
 // The smaller tiles are bound by the instructions a wavefront issues per block (its 32 additions per 8 products first of all), 256 x 256 by power.
 struct TileShape {
     int rows, toks, per_cu;
@@ -540,8 +548,8 @@ struct TileShape {
 };
 constexpr TileShape kTiles[] = {{256, 256, 1, 1.7f, 1.3f},   {256, 128, 1, 1.0f, 0.8f},  {128, 128, 1, 0.62f, 0.5f},
                                 {64, 128, 1, 0.40f, 0.38f}, {64, 64, 2, 0.45f, 0.33f}, {64, 64, 1, 0.24f, 0.24f}};
-// (with results in fp32: 128 x 128, the same by two groups, 64 x 128 and 64 x 64 by two groups; 333 tokens on 10007 x 4100: 42, [38], 49, 65;
-// 1024 tokens on 11008 x 4096: [90], 98, 133, 167; 128 tokens on 4096 x 4096: 39, 32, 23, [16])
+// (with results in fp32: 128 x 128, the same by two groups, 64 x 128 and 64 x 64 by two groups; 128 tokens on 4096 x 4096: 37, 31, 23, [16]; 256 tokens on
+// 5120 x 5120: 45, 37, [28], 35; 333 tokens on 10007 x 4100: 40, [36], 48, 61; 1024 tokens on 11008 x 4096: [89], 94, 131, 154)
 constexpr TileShape kExactTiles[] = {{128, 128, 2, 1.31f, 1.1f}, {128, 128, 1, 0.97f, 0.92f}, {64, 128, 1, 0.64f, 0.64f}, {64, 64, 1, 0.42f, 0.42f}};
 
 static int plan_tile(const BlockGemmArgs &a, bool exact)
