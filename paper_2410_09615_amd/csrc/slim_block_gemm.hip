@@ -229,8 +229,10 @@ __global__ __launch_bounds__(THREADS) void block_stream_kernel(BlockGemmArgs a)
 // Results leave through LDS, so that a store instruction writes whole lines of a token's row.
 // 28672 x 8192 at 4096 tokens takes 760 to 782 us from card to card, 2.53 PFLOP/s (671 us for the library's product with one scale in all): power holds the clock at 1.65 GHz,
 // the matrix pipes are busy 68 % of it; without the scaled additions, 4 of a lane's instructions per product, it would be 661, without
-// loads 595.  10007 x 4100 at 333 tokens in fp32 (EXACT) takes 35.3 us at 2.4 GHz, matrix pipes 32 % busy: chains of four products and the conversions
-// between them; chains of two products issued in turn by hand were no faster (35.4).
+// loads 595.  10007 x 4100 at 333 tokens in fp32 (EXACT) takes 35.3 us, matrix pipes 32 % busy: its 128 conversions and 64 additions per 64 products
+// of a wavefront take about as long to issue as the products, and hide behind them only in part (without the conversions 26.7 us, without the
+// additions 25.7, without the products 26.4, without loads 32.7); a conversion and an addition placed by hand after every product, or two chains of
+// products in turn, were no faster (36.4, 37.5).
 // KG = 2: two such groups of wavefronts share the tile, each with half of the blocks and buffers of its own, and their sums are added at the end: where
 // there are few tiles, twice the loads are under way, and a SIMD has two wavefronts with the larger share of the tile.
 template <int BM, int BN, int STAGES>
@@ -337,7 +339,10 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
     auto place = [](int i) { return i < MAIN || TAIL == 1 ? i % 2 : 2 + i - MAIN; };
     Codes<false> x[BF], wv[WBUF];
     float s[BF], wsb;
-    // EXACT: what is being multiplied as fp16 numbers, made of the codes when the products begin (by then they are there)
+    // EXACT: what is being multiplied as fp16 numbers, made of the codes when the products begin (by then they are there); or, of AHEAD tokens' tiles,
+    // among the last products of the block before, a tile after its codes were asked for.  With one group: 1024 tokens on 11008 x 4096 89.3 -> 86.9 us,
+    // 4096 tokens on 8192 x 8192 470 -> 458.  With two, whose wavefronts fill in for each other, it loses 1 %.
+    constexpr int AHEAD = KG == 1 ? BF - 1 : 0;
     Codes<true> xh[EXACT ? BF : 1], wh[EXACT ? TAIL : 1];
     auto product = [&](int i, int t) {
         if constexpr (EXACT)
@@ -377,6 +382,10 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
         s[t] = load_scale(0, t) * wsb;
     }
     wv[0] = load_w(0, 0);
+    if constexpr (EXACT) {
+#pragma unroll
+        for (int t = 0; t < AHEAD; ++t) xh[t] = Codes<true>(x[t].h[0], x[t].h[1]);
+    }
 
     for (int b = 0, buffer = 0; b < turns; ++b) {
         const int after = buffer + 1 < STAGES ? buffer + 1 : 0, before = buffer > 0 ? buffer - 1 : STAGES - 1;
@@ -387,7 +396,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
                 if constexpr (TAIL > 1 && i >= MAIN - TAIL) wv[place(i + TAIL)] = load_w(buffer, i + TAIL);
                 if constexpr (EXACT) wh[0] = Codes<true>(wv[place(i)].h[0], wv[place(i)].h[1]);
             }
-            if constexpr (EXACT && i == 0) xh[t] = Codes<true>(x[t].h[0], x[t].h[1]);
+            if constexpr (EXACT && i == 0 && t >= AHEAD) xh[t] = Codes<true>(x[t].h[0], x[t].h[1]);
             if constexpr (n % SPREAD == 0 && EARLY + n / SPREAD < UNITS)
                 fetch_unit(std::integral_constant<int, EARLY + n / SPREAD>{}, b + STAGES - 1, before);
             if constexpr (n >= LAG) add(std::integral_constant<int, n - LAG>{});
@@ -421,6 +430,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
                 fetch_unit(std::integral_constant<int, (n - MAIN * BF) / SPREAD>{}, b + STAGES, buffer);
             p[n % (LAG + 1)] = product(i, t);
             if constexpr (i == AF - 1) x[t] = load_x(after, t);
+            if constexpr (EXACT && i == AF - 1 && t > 0 && t <= AHEAD) xh[t - 1] = Codes<true>(x[t - 1].h[0], x[t - 1].h[1]);
             add(std::integral_constant<int, n - LAG>{});
             if constexpr (!EXACT || n % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         });
@@ -549,7 +559,7 @@ struct TileShape {
 constexpr TileShape kTiles[] = {{256, 256, 1, 1.7f, 1.3f},   {256, 128, 1, 1.0f, 0.8f},  {128, 128, 1, 0.62f, 0.5f},
                                 {64, 128, 1, 0.40f, 0.38f}, {64, 64, 2, 0.45f, 0.33f}, {64, 64, 1, 0.24f, 0.24f}};
 // (with results in fp32: 128 x 128, the same by two groups, 64 x 128 and 64 x 64 by two groups; 128 tokens on 4096 x 4096: 37, 31, 23, [16]; 256 tokens on
-// 5120 x 5120: 45, 37, [28], 35; 333 tokens on 10007 x 4100: 40, [36], 48, 61; 1024 tokens on 11008 x 4096: [89], 94, 131, 154)
+// 5120 x 5120: 45, 37, [28], 35; 333 tokens on 10007 x 4100: 40, [36], 48, 61; 1024 tokens on 11008 x 4096: [87], 94, 131, 154)
 constexpr TileShape kExactTiles[] = {{128, 128, 2, 1.31f, 1.1f}, {128, 128, 1, 0.97f, 0.92f}, {64, 128, 1, 0.64f, 0.64f}, {64, 64, 1, 0.42f, 0.42f}};
 
 static int plan_tile(const BlockGemmArgs &a, bool exact)
