@@ -67,14 +67,17 @@ __device__ __forceinline__ void load_piece(const typename T::type *row, int at, 
         for (int e = 0; e < N; ++e) v[e] = at + e < len ? (float)row[at + e] : 0.f;
     }
 }
-template <class T, int N>
+template <class T, int N, bool STREAMING = false>
 __device__ __forceinline__ void store_piece(typename T::type *row, int at, int len, const float (&v)[N])
 {
     if (at + N <= len) {
         typename Piece<T, N>::vec x;
 #pragma unroll
         for (int e = 0; e < N; ++e) x[e] = (typename T::type)v[e];
-        Piece<T, N>::store(row + at, x);
+        if constexpr (STREAMING)
+            Piece<T, N>::store_streaming(row + at, x);
+        else
+            Piece<T, N>::store(row + at, x);
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e)

@@ -81,8 +81,9 @@ __device__ __forceinline__ void gain_piece(const NormArgs &a, int at, float (&g)
 
 // A row per workgroup, NV pieces of 8 values per lane, held in registers from the one read to the last write (more rows than
 // workgroups fit into a grid are walked).  LONG: rows that do not fit so are read twice, the sum first.
-// Bound by memory: 4096 x 8192 in fp16 with a residual moves 236 MB in 49 us, 4.8 TB/s (a large copy: 5.15); 1777 x 5003 in bf16, whose rows begin
-// at odd elements, 80 MB in 19.7 us (13 % of it for that).  One row of 8192 takes 3.7 us: the launch, one read, the sum across
+// Bound by memory: 4096 x 8192 in fp16 with a residual moves 236 MB in 46 us, 5.1 TB/s (a large copy: 5.15); 1777 x 5003 in bf16, whose rows begin
+// at odd elements, 80 MB in 18.8 us (13 % of it for that).  H, which nothing reads soon, is stored past the caches' turn (49.4 and 19.5 us without that); the codes are not:
+// it would be 44.8 here and 9 us more in the product that reads them (the feed-forward part of 4096 x 11008 at 512 tokens 108 -> 117 us).  One row of 8192 takes 3.7 us: the launch, one read, the sum across
 // wavefronts, one write.  Workgroups that stay and walk the rows with the next row's loads under way, 2 to 32 of them per compute unit, took 48 to 57 us.
 // 1 / sqrt and not the approximation: once per row.
 template <class T, int NV, bool LONG>
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a)
                     gain_piece<T>(a, at, g);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum += z[p][e] * z[p][e];
-                    if (a.H) store_piece<T>(static_cast<E *>(a.H) + row * a.h_ld, at, a.k, z[p]);
+                    if (a.H) store_piece<T, 8, true>(static_cast<E *>(a.H) + row * a.h_ld, at, a.k, z[p]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) z[p][e] *= g[e];
                     sc[p] = encode(row, at, z[p]);
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a)
             const float rstd = factor(sum);
             for (int at = first; at < kp; at += step) {
                 norm_load<T>(a, row, at, h);            // (H or Y may be X or the residual: a piece is read and written by one lane, here last)
-                if (a.H) store_piece<T>(static_cast<E *>(a.H) + row * a.h_ld, at, a.k, h);
+                if (a.H) store_piece<T, 8, true>(static_cast<E *>(a.H) + row * a.h_ld, at, a.k, h);
                 gain_piece<T>(a, at, g);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) h[e] *= g[e];
@@ -196,6 +197,7 @@ struct ActArgs {
 // 16 lanes per block.  A lane takes one piece per round; nothing is shared between blocks, so the largest of a block is found in registers and the
 // values are read once.  Bound by memory: 2048 x 11008 in bf16, gated, moves 114 MB in 23 us, 5.0 TB/s (a large copy: 5.15); 16 x 13824 takes
 // 3.0 us, a launch and one dependent access.  exp and the division in 32 bits; the result is rounded once, to its code.
+// (Codes stored past the caches' turn: 23 us, and as much more in the product that reads them at 512 tokens.)
 template <class T, bool SILU>
 __global__ __launch_bounds__(256) void act_kernel(ActArgs a)
 {
@@ -230,8 +232,8 @@ __device__ __forceinline__ uint32_t wtile_lds(uint32_t place)
 }
 
 // One workgroup per 128 x 128 weights: in registers while their largest is found (so they are read once), then through LDS into the order of the tiles.
-// VEC values of 16 bytes per lane and load.  Bound by memory: 28672 x 8192 in bf16 moves 705 MB in 129 us, 5.5 TB/s (a large copy: 5.15, half of it
-// writes; here a third); 4096 x 4096 in fp32 84 MB in 14.5 us.
+// VEC values of 16 bytes per lane and load.  Bound by memory: 28672 x 8192 in bf16 moves 705 MB in 123 us, 5.7 TB/s (a large copy: 5.15, half of it
+// writes; here a third); 4096 x 4096 in fp32 84 MB in 14.2 us.  The codes are stored past the caches' turn (128 and 14.4 us without; loads so are slower, 16 us the second).
 template <class T>
 __global__ __launch_bounds__(256) void weight_kernel(const typename T::type *W, int64_t ld, int n, int k, int kb, uint8_t *codes, float *scales)
 {
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(256) void weight_kernel(const typename T::type *W, 
 #pragma unroll
         for (int s = 0; s < kWTileBytes / 4096; ++s) {
             const uint32_t at = (uint32_t)s * 4096u + threadIdx.x * 16u;
-            *reinterpret_cast<uint4_t *>(out + at) = *reinterpret_cast<const uint4_t *>(tile + wtile_lds((uint32_t)u * kWTileBytes + at));
+            __builtin_nontemporal_store(*reinterpret_cast<const uint4_t *>(tile + wtile_lds((uint32_t)u * kWTileBytes + at)), reinterpret_cast<uint4_t *>(out + at));
         }
     }
 }
