@@ -292,16 +292,19 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
             load_to_lds(sd, soff[i] + (uint32_t)(first + b) * 4u, 0u, lds0 + Lds::scales + (uint32_t)(b >> 4 & 1) * Lds::chunk + (uint32_t)(w * SL + i) * 1024u);
     };
     // Unit `u` of this wavefront's share of the group's block b.  Past the last block nothing is read (from a buffer of no length; zeros): the number of
-    // loads under way is the same everywhere.
+    // loads under way is the same everywhere.  The uniform offset is then 0: whether the range check leaves it out or takes it off the buffer's length, 0
+    // bytes from there on are no bytes, and no address is one of a neighbour's block or past the operand.
     auto fetch_unit = [&](auto uc, int b, int buffer) {
         constexpr int u = decltype(uc)::value;
         const uint32_t base = lds0 + (uint32_t)buffer * Lds::stage;
+        const bool there = b < count;
+        const uint32_t block = there ? (uint32_t)(first + b) : 0u;
         if constexpr (u < WU) {
-            const rsrc_t d = make_rsrc(wbase, b < count ? (uint32_t)rows * kp : 0u);
-            load_run_to_lds<RUN, u * RUN * 1024>(d, woff[u], (uint32_t)(first + b) * kWTileBytes, base + (uint32_t)(w * WL) * 1024u);
+            const rsrc_t d = make_rsrc(wbase, there ? (uint32_t)rows * kp : 0u);
+            load_run_to_lds<RUN, u * RUN * 1024>(d, woff[u], block * kWTileBytes, base + (uint32_t)(w * WL) * 1024u);
         } else {
-            const rsrc_t d = make_rsrc(xbase, b < count ? (uint32_t)toks * kp : 0u);
-            load_run_to_lds<1, WB + (u - WU) * 1024>(d, xoff[u - WU], (uint32_t)(first + b) * kBlk, base + (uint32_t)(w * XL) * 1024u);
+            const rsrc_t d = make_rsrc(xbase, there ? (uint32_t)toks * kp : 0u);
+            load_run_to_lds<1, WB + (u - WU) * 1024>(d, xoff[u - WU], block * kBlk, base + (uint32_t)(w * XL) * 1024u);
         }
     };
 

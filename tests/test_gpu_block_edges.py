@@ -1,0 +1,61 @@
+"""The product of 8-bit inputs and weights where its loads and its two groups of wavefronts end: what lies behind a row's last block.
+
+Bounds as in test_gpu_block_fp8.py: (128 + kb + 18) 2^-24 of the sum of the terms' magnitudes, above 64 tokens and in 16 bits 2^-10 of it more
+(the 8-bit instruction's cut), and one rounding to the result's type.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_fp8 as O
+from paper_2410_09615_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+HALF_ULP = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8, torch.float32: U}
+NAN = 0x7F
+
+
+def _codes(rows, cols, g):
+    c = g.integers(0, 256, (rows, cols), dtype=np.uint8)
+    c[(c & 0x7F) == 0x7F] = 0x3A
+    return c
+
+
+def _run(xc, xs, wc, ws, dtype):
+    layer = B.SlimBlockFp8Weight(*wc.shape, B.slim_block_fp8_tile(torch.from_numpy(wc).to(DEV)), torch.from_numpy(ws).to(DEV))
+    return B.slim_block_fp8_gemm(layer, torch.from_numpy(xc).to(DEV), torch.from_numpy(xs).to(DEV), dtype).double().cpu().numpy()
+
+
+def _check(got, xc, xs, wc, ws, dtype):
+    """Finite results within the bound, the others as the definition has them."""
+    with np.errstate(all="ignore"):
+        ref, mag = O.gemm(xc, xs, wc, ws)
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    endless = np.isinf(ref)
+    assert np.array_equal(got[endless], ref[endless])
+    fine = np.isfinite(ref)
+    bound = (128 + xs.shape[1] + 18) * U * mag
+    if dtype != torch.float32 and got.shape[0] > 64:
+        bound = bound + 2.0 ** -10 * mag
+    assert np.all(np.abs(got - ref)[fine] <= (bound + HALF_ULP[dtype] * (np.abs(ref) + bound))[fine])
+
+
+# one block (the second group has none), odd numbers of blocks (it has one less), more than the scales of one fetch
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("kb", [1, 3, 5, 17, 33])
+@pytest.mark.parametrize("m", [3, 70, 130, 257])
+def test_nothing_of_the_next_token_or_row_tile(m, kb, dtype):
+    """The first block of every other token and of every other 64 rows, which lies behind the last block of the one before, is all NaN."""
+    n, k = 300, kb * 128
+    g = np.random.default_rng(m + kb)
+    wc, xc = _codes(n, k, g), _codes(m, k, g)
+    for t in range(64, n, 128):
+        wc[t:t + 64, :128] = NAN
+    xc[1::2, :128] = NAN
+    ws = (2.0 ** g.uniform(-9, -6, (O.blocks(n), kb))).astype(np.float32)
+    xs = (2.0 ** g.uniform(-9, -6, (m, kb))).astype(np.float32)
+    got = _run(xc, xs, wc, ws, dtype)
+    assert np.isfinite(got[0::2, :64]).all() and np.isnan(got[1::2]).all()
+    _check(got, xc, xs, wc, ws, dtype)
