@@ -25,6 +25,8 @@ HIPCC_FLAGS = [
     # m0 is a register the compiler keeps no value in; asm that writes it names it all the same, so that the
     # compiler's own uses stay in order with it, and would be warned about each time.
     "-Wall", "-Wno-unused-function", "-Wno-inline-asm",
+    # a constant index outside a register array: whatever is written there is lost without a trace
+    "-Werror=array-bounds",
 ]
 
 

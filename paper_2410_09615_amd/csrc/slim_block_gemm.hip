@@ -435,7 +435,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
             p[n % (LAG + 1)] = product(i, t);
             if constexpr (i == AF - 1) x[t] = load_x(after, t);
             if constexpr (EXACT && i == AF - 1 && t > 0 && t <= AHEAD) xh[t - 1] = Codes<true>(x[t - 1].h[0], x[t - 1].h[1]);
-            add(std::integral_constant<int, n - LAG>{});
+            if constexpr (n >= LAG) add(std::integral_constant<int, n - LAG>{});        // (64 x 64: the third product is the tail's first)
             if constexpr (!EXACT || n % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         });
         static_for<LAG>([&](auto nc) { add(std::integral_constant<int, SLOTS - LAG + decltype(nc)::value>{}); });
