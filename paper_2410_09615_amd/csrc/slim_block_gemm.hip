@@ -270,7 +270,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
     const float *ws = a.ws + (int64_t)rb * a.kb;
     uint8_t *const own = lds + group * Lds::bytes;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)own;
-    // the group's blocks: count from `first` on (none where there is one block only), in as many turns as any group's
+    // the group's blocks: count from `first` on; the second group may have one less than the first (none where there is one block only)
     const int turns = (a.kb + KG - 1) / KG, first = group * turns, count = min(turns, a.kb - first);
 
     // this wavefront's shares of a block: a run of KiB of the weight tiles, and groups of eight tokens whose eight 16-byte pieces are put in another
@@ -327,10 +327,8 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
         return Codes<false>(*reinterpret_cast<const uint4_t *>(frag), *reinterpret_cast<const uint4_t *>(frag + 1024));
     };
     auto load_scale = [&](int b, int t) {
-        const float v = *reinterpret_cast<const float *>(own + Lds::scales + (b >> 4 & 1) * Lds::chunk + ((wt * BF + t) * 16 + j) * 64 +
-                                                         ((b >> 2 & 3) ^ (j >> 2)) * 16 + (b & 3) * 4);
-        // (a group that has a block less than the other adds nothing in the last turn, whatever is there)
-        return KG == 1 || b < count ? v : 0.f;
+        return *reinterpret_cast<const float *>(own + Lds::scales + (b >> 4 & 1) * Lds::chunk + ((wt * BF + t) * 16 + j) * 64 +
+                                                ((b >> 2 & 3) ^ (j >> 2)) * 16 + (b & 3) * 4);
     };
 
     float4_t acc[AF][BF];
@@ -391,7 +389,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
         for (int t = 0; t < AHEAD; ++t) xh[t] = Codes<true>(x[t].h[0], x[t].h[1]);
     }
 
-    for (int b = 0, buffer = 0; b < turns; ++b) {
+    for (int b = 0, buffer = 0; b < count; ++b) {
         const int after = buffer + 1 < STAGES ? buffer + 1 : 0, before = buffer > 0 ? buffer - 1 : STAGES - 1;
         static_for<MAIN * BF>([&](auto nc) {
             constexpr int n = decltype(nc)::value, i = row_of(n), t = token_of(n);
@@ -443,6 +441,9 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
         for (int t = 0; t < BF; ++t) s[t] = sn[t] * wsb;
         buffer = after;
     }
+    // A group with a block less has nothing to multiply in the last turn, where the other meets its barrier once more.  (Not zeros with a scale of 0: that
+    // times an infinite scale of the rows' last block is a NaN, and what is not there need not be zeros.)
+    if (KG > 1 && count < turns) __builtin_amdgcn_s_barrier();
 
     // Results stream past the caches where their rows begin at multiples of 64 bytes; otherwise the ends of a tile's rows are parts of lines, which are better
     // put together in the L2.  (2171 x 7424 and x 7442 in fp32 on 166 inputs: 17.6 and 27.8 us streaming, 20.0 and 21.2 cached; 4096 x 11008 on 512: 65 and 85.)

@@ -59,3 +59,33 @@ def test_nothing_of_the_next_token_or_row_tile(m, kb, dtype):
     got = _run(xc, xs, wc, ws, dtype)
     assert np.isfinite(got[0::2, :64]).all() and np.isnan(got[1::2]).all()
     _check(got, xc, xs, wc, ws, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("kb", [1, 3, 5, 17])
+@pytest.mark.parametrize("m", [3, 70, 130, 257])
+def test_an_infinite_scale_of_the_last_block(m, kb, dtype):
+    """sum_b xs ws (sum of the block): a block's sum is a number, so its infinite scale gives an infinity of the sum's sign and no NaN
+    (where the sum is further from zero than its own error)."""
+    n, k = 300, kb * 128
+    g = np.random.default_rng(100 * m + kb)
+    wc, xc = _codes(n, k, g), _codes(m, k, g)
+    ws = (2.0 ** g.uniform(-9, -6, (O.blocks(n), kb))).astype(np.float32)
+    xs = (2.0 ** g.uniform(-9, -6, (m, kb))).astype(np.float32)
+    ws[1, kb - 1] = np.inf
+    xs[m - 1, kb - 1] = np.inf
+    X, W = O.values(xc), O.values(wc)
+    last, size = X[:, -128:] @ W[:, -128:].T, np.abs(X[:, -128:]) @ np.abs(W[:, -128:]).T
+    cut = 128 * U + (2.0 ** -10 if dtype != torch.float32 and m > 64 else 0)
+    got = _run(xc, xs, wc, ws, dtype)
+    endless = np.zeros((m, n), bool)
+    endless[:, 128:256] = True
+    endless[m - 1] = True
+    sure = endless & (np.abs(last) > cut * size)
+    assert sure.sum() > 0.9 * endless.sum()
+    assert np.array_equal(got[sure], np.copysign(np.inf, last)[sure]) and np.isfinite(got[~endless]).all()
+    ws[1, kb - 1] = xs[m - 1, kb - 1] = 0
+    got[endless] = 0
+    ref, mag = O.gemm(xc, xs, wc, ws)
+    bound = (128 + kb + 18) * U * mag + (2.0 ** -10 * mag if dtype != torch.float32 and m > 64 else 0)
+    assert np.all((np.abs(got - ref) <= bound + HALF_ULP[dtype] * (np.abs(ref) + bound))[~endless])
