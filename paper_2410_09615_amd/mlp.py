@@ -38,8 +38,8 @@ class DecoderMlp:
         self._a, self._as = byte(max_tokens, fb * 128), real(max_tokens, fb)
         self._gu = half(max_tokens, 2 * self.f)
         self._y = half(max_tokens, self.k) if self.packed else None
-        if self.packed:        # decode calls and prompts need different room
-            room = max(slim.slim_workspace_bytes(gate_up, m) for m in (min(max_tokens, 16), max_tokens))
+        if self.packed:        # what a call needs does not grow with its tokens throughout: the most that any number of them does
+            room = max(slim.slim_workspace_bytes(gate_up, m) for m in range(1, max_tokens + 1))
             self._ws = torch.zeros(room, dtype=torch.uint8, device=dev)
         else:
             self._ws = slim.alloc_block_fp8_workspace(gate_up, max_tokens)
