@@ -50,6 +50,8 @@ class DecoderMlp:
         m = X.shape[0]
         if m > self.max_tokens:
             raise ValueError(f"{m} tokens, made for {self.max_tokens}")
+        if X.dtype is not torch.float16:
+            raise ValueError("X must be float16")
         gu = self._gu[:m]
         codes, scales, h, y = slim.slim_block_fp8_norm(X, self.gain, self.eps, residual=residual, codes=self._x[:m], scales=self._xs[:m],
                                                        H=True if h is None else h, Y=self._y[:m] if self.packed else None)

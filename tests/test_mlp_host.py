@@ -28,3 +28,11 @@ def test_workspace_beside_a_layer_in_4_bits_covers_every_number_of_tokens(f, k, 
     mlp = DecoderMlp(torch.ones(k), layer, _down(k, f), tokens)
     need = [B.slim_workspace_bytes(layer, m) for m in range(1, tokens + 1)]
     assert mlp._ws.numel() >= max(need)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_takes_fp16_only(dtype):
+    """Its inner matrices and what it returns are fp16: other inputs would come back in a type beside theirs."""
+    mlp = DecoderMlp(torch.ones(256), _packed(512, 256, 32), _down(256, 256), 4)
+    with pytest.raises(ValueError, match="float16"):
+        mlp(torch.zeros(2, 256, dtype=dtype))
