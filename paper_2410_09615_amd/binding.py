@@ -184,6 +184,10 @@ class SlimLayer:
         self.__dict__.pop("_ref", None)
         object.__setattr__(self, name, value)
 
+    def __getstate__(self):
+        """The fields: a copy or a stored layer has buffers of its own, and makes its own reference to them."""
+        return {name: value for name, value in self.__dict__.items() if name != "_ref"}
+
 
 def slim_pack(W: torch.Tensor, qvals=None, meta=None, scale=None):
     """W fp32 [n][k] on the device -> (qvals, meta, scale) device tensors."""
@@ -741,6 +745,10 @@ class SlimBlockFp8Weight:
     def __setattr__(self, name, value):
         self.__dict__.pop("_ref", None)
         object.__setattr__(self, name, value)
+
+    def __getstate__(self):
+        """The fields: a copy or a stored layer has buffers of its own, and makes its own reference to them."""
+        return {name: value for name, value in self.__dict__.items() if name != "_ref"}
 
 
 def compress_block_fp8(W: torch.Tensor) -> SlimBlockFp8Weight:
