@@ -717,6 +717,8 @@ class _LayerRef:
     layer: slim_block_fp8_layer
     address: int
     device: int
+    codes: tuple           # (address, elements)
+    scales: tuple
 
 
 @dataclass
@@ -729,16 +731,19 @@ class SlimBlockFp8Weight:
 
     def c_ref(self):
         """What the product is given of the layer; the buffers are checked when it is made, once per layer and again after any field is
-        assigned."""
+        assigned or a tensor has other data."""
+        c, s = self.codes, self.scales
+        at = (c.data_ptr(), c.numel()), (s.data_ptr(), s.numel())
         ref = self.__dict__.get("_ref")
-        if ref is None:
+        if ref is None or (ref.codes, ref.scales) != at:
+            self.__dict__.pop("_ref", None)
             size = slim_block_fp8_weight_sizes(self.n, self.k)
-            _dev(self.codes, torch.uint8, "codes")
-            _dev(self.scales, torch.float32, "scales")
-            if self.codes.numel() != size["codes"] or self.scales.numel() * 4 != size["scales"] or self.scales.device != self.codes.device:
+            _dev(c, torch.uint8, "codes")
+            _dev(s, torch.float32, "scales")
+            if c.numel() != size["codes"] or s.numel() * 4 != size["scales"] or s.device != c.device:
                 raise ValueError("codes and scales are not an n x k layer's on one device")
-            cs = slim_block_fp8_layer(self.n, self.k, self.codes.data_ptr(), self.scales.data_ptr())
-            ref = _LayerRef(cs, ctypes.addressof(cs), self.codes.get_device())
+            cs = slim_block_fp8_layer(self.n, self.k, c.data_ptr(), s.data_ptr())
+            ref = _LayerRef(cs, ctypes.addressof(cs), c.get_device(), *at)
             self.__dict__["_ref"] = ref
         return ref
 

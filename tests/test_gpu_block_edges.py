@@ -89,3 +89,25 @@ def test_an_infinite_scale_of_the_last_block(m, kb, dtype):
     ref, mag = O.gemm(xc, xs, wc, ws)
     bound = (128 + kb + 18) * U * mag + (2.0 ** -10 * mag if dtype != torch.float32 and m > 64 else 0)
     assert np.all((np.abs(got - ref) <= bound + HALF_ULP[dtype] * (np.abs(ref) + bound))[~endless])
+
+
+def test_a_layer_whose_buffers_were_exchanged():
+    """`.data` of a layer's tensors exchanged between products (weights reloaded or moved): the next product is on what is there now."""
+    g = np.random.default_rng(5)
+    wc, xc = _codes(70, 200, g), _codes(5, 256, g)
+    xc[:, 200:] = 0
+    ws, xs = np.full((1, 2), 0.25, np.float32), np.full((5, 2), 0.5, np.float32)
+    X, S = torch.from_numpy(xc).to(DEV), torch.from_numpy(xs).to(DEV)
+    layer = B.SlimBlockFp8Weight(70, 200, B.slim_block_fp8_tile(torch.from_numpy(wc).to(DEV)), torch.from_numpy(ws).to(DEV))
+    first = layer.codes.data, layer.scales.data                        # (still there while the second product runs)
+    _check(B.slim_block_fp8_gemm(layer, X, S, torch.float32).double().cpu().numpy(), xc, xs, wc, ws, torch.float32)
+    wc = wc[::-1].copy()
+    layer.codes.data = B.slim_block_fp8_tile(torch.from_numpy(wc).to(DEV))
+    _check(B.slim_block_fp8_gemm(layer, X, S, torch.float32).double().cpu().numpy(), xc, xs, wc, ws, torch.float32)
+    ws = 2 * ws
+    layer.scales.data = torch.from_numpy(ws).to(DEV)
+    _check(B.slim_block_fp8_gemm(layer, X, S, torch.float32).double().cpu().numpy(), xc, xs, wc, ws, torch.float32)
+    layer.scales.data = layer.scales.data[:, :1].contiguous()
+    with pytest.raises(ValueError):
+        B.slim_block_fp8_gemm(layer, X, S, torch.float32)
+    del first
