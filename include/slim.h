@@ -560,10 +560,9 @@ typedef struct {
  * sums in binary32, Y [m][n] rounded once to `dtype` (any slim_dtype), row stride y_ld.
  * The inputs' codes and scales are slim_block_fp8_norm's or slim_block_fp8_act's (or the caller's own, in
  * their layout).  Results do not depend on the order of workgroups.
- * workspace: slim_block_fp8_gemm_workspace (HOST out-pointer; the size for m covers every smaller m), ZERO-FILLED
- * ONCE before its first use; one for calls that follow one another, two for calls that overlap.  (256 bytes at any
- * size: every kernel here adds its partial sums up inside a workgroup, and none keeps anything in it.  It is there
- * so that a product whose workgroups share a sum can be added without a change for the caller.)
+ * workspace: slim_block_fp8_gemm_workspace (HOST out-pointer; the size for m covers every smaller m): 256 bytes at any
+ * size.  No kernel reads or writes it -- each adds its partial sums up inside a workgroup -- so it need not be filled and
+ * calls that overlap may share one.
  * Enqueues kernels only and may be captured into a HIP graph.
  * Errors: NULL, SHAPE, ALIGN, WORKSPACE, HIP.
  */

@@ -768,7 +768,7 @@ def slim_block_fp8_gemm_workspace(n: int, k: int, m: int) -> int:
 
 
 def alloc_block_fp8_workspace(layer: SlimBlockFp8Weight, m: int) -> torch.Tensor:
-    return torch.zeros(slim_block_fp8_gemm_workspace(layer.n, layer.k, m), dtype=torch.uint8, device=layer.codes.device)
+    return torch.empty(slim_block_fp8_gemm_workspace(layer.n, layer.k, m), dtype=torch.uint8, device=layer.codes.device)
 
 
 def slim_block_fp8_gemm(layer: SlimBlockFp8Weight, codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.float16, Y=None,

@@ -111,3 +111,31 @@ def test_a_layer_whose_buffers_were_exchanged():
     with pytest.raises(ValueError):
         B.slim_block_fp8_gemm(layer, X, S, torch.float32)
     del first
+
+
+def test_a_product_without_a_workspace_enqueues_nothing_else():
+    """The default workspace is an allocation and no more: nothing reads it, so nothing fills it."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Names(TorchDispatchMode):
+        def __init__(self):
+            super().__init__()
+            self.seen = []
+
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            self.seen.append(func.overloadpacket.__name__)
+            return func(*args, **(kwargs or {}))
+
+    g = np.random.default_rng(7)
+    wc, xc = _codes(70, 256, g), _codes(2, 256, g)
+    ws, xs = np.full((1, 2), 0.25, np.float32), np.full((2, 2), 0.5, np.float32)
+    X, S = torch.from_numpy(xc).to(DEV), torch.from_numpy(xs).to(DEV)
+    layer = B.SlimBlockFp8Weight(70, 256, B.slim_block_fp8_tile(torch.from_numpy(wc).to(DEV)), torch.from_numpy(ws).to(DEV))
+    with Names() as names:
+        Y = B.slim_block_fp8_gemm(layer, X, S, torch.float32)
+    _check(Y.double().cpu().numpy(), xc, xs, wc, ws, torch.float32)
+    assert set(names.seen) <= {"empty"}, names.seen
+    for fill in (0, 0xFF):                              # whatever is in one
+        full = torch.full((B.slim_block_fp8_gemm_workspace(70, 256, 2),), fill, dtype=torch.uint8, device=DEV)
+        assert torch.equal(B.slim_block_fp8_gemm(layer, X, S, torch.float32, workspace=full), Y)
+        assert bool((full == fill).all())
