@@ -191,7 +191,7 @@ static PyObject *gemm(PyObject *self, PyObject *const *a, Py_ssize_t n)
     int status;
     const long long kb = ((long long)layer->k + 127) / 128;
     if (rows(a[2], "codes", &c)) return NULL;
-    if ((c.type != U8 && c.type != E4M3) || c.device != device || c.k != kb * 128 || c.ld != c.k)
+    if ((c.type != U8 && c.type != E4M3) || c.device != device || c.k != kb * 128 || (c.m > 1 && c.ld != c.k))
         return refuse("codes", "must be contiguous uint8 [m][128 ceil(k / 128)] on the layer's device"), NULL;
     if (whole(a[3], "scales", SLIM_F32, SLIM_F32, c.m * kb, device, &scales)) return NULL;
     if (rows(a[4], "Y", &y)) return NULL;

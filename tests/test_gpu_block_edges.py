@@ -139,3 +139,20 @@ def test_a_product_without_a_workspace_enqueues_nothing_else():
         full = torch.full((B.slim_block_fp8_gemm_workspace(70, 256, 2),), fill, dtype=torch.uint8, device=DEV)
         assert torch.equal(B.slim_block_fp8_gemm(layer, X, S, torch.float32, workspace=full), Y)
         assert bool((full == fill).all())
+
+
+def test_one_token_of_a_wider_matrix():
+    """A single row of codes has no gaps, whatever its stride says (torch calls it contiguous too); two rows of one have."""
+    g = np.random.default_rng(9)
+    wc, xc = _codes(70, 200, g), _codes(2, 256, g)
+    xc[:, 200:] = 0
+    ws, xs = np.full((1, 2), 0.25, np.float32), np.full((2, 2), 0.5, np.float32)
+    layer = B.SlimBlockFp8Weight(70, 200, B.slim_block_fp8_tile(torch.from_numpy(wc).to(DEV)), torch.from_numpy(ws).to(DEV))
+    wide, S = torch.zeros(2, 512, dtype=torch.uint8, device=DEV), torch.from_numpy(xs).to(DEV)
+    wide[:, 256:] = torch.from_numpy(xc).to(DEV)
+    one = wide[1:, 256:]
+    assert one.is_contiguous()
+    Y = B.slim_block_fp8_gemm(layer, one, S[1:], torch.float32)
+    _check(Y.double().cpu().numpy(), xc[1:], xs[1:], wc, ws, torch.float32)
+    with pytest.raises(ValueError):
+        B.slim_block_fp8_gemm(layer, wide[:, 256:], S, torch.float32)
