@@ -571,6 +571,14 @@ int slim_block_fp8_gemm(const slim_block_fp8_layer *layer, const uint8_t *X, con
                         int64_t y_ld, int32_t dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * slim_block_fp8_gemm_plan -- what slim_block_fp8_gemm would launch on the current device, for inspection and tests (no
+ * launch): out int32 [6] (HOST) = kernel (0: weights streamed, up to 64 tokens; 1: tiles), rows and tokens of a
+ * workgroup's tile, its threads, workgroups, and 1 where products are summed in binary32 (0: by the 8-bit instruction).
+ * Errors: NULL, SHAPE.
+ */
+int slim_block_fp8_gemm_plan(int32_t n, int32_t k, int32_t m, int32_t dtype, int32_t *out);
+
+/*
  * Measurement aids (they compute nothing of the method): what this machine
  * delivers on a plain streaming read and on back-to-back matrix instructions,
  * to set beside the nominal peaks when a kernel's roofline fraction is quoted

@@ -48,7 +48,8 @@ EXPORTS = ["slim_status_string", "slim_rank_pad", "slim_packed_sizes", "slim_pac
            "slim_compute_adapters", "slim_input_quant_fp8", "slim_probe_read", "slim_probe_mfma", "slim_gemm_tile_order", "slim_input_quant_fp8_codes",
            "slim_linear_gemm_fp8",
            "slim_block_fp8_sizes", "slim_block_fp8_weight_sizes", "slim_block_fp8_norm", "slim_block_fp8_act", "slim_block_fp8_weight",
-           "slim_block_fp8_tile", "slim_block_fp8_untile", "slim_block_fp8_gemm_workspace", "slim_block_fp8_gemm"]
+           "slim_block_fp8_tile", "slim_block_fp8_untile", "slim_block_fp8_gemm_workspace", "slim_block_fp8_gemm",
+           "slim_block_fp8_gemm_plan"]
 
 
 def lib():
@@ -102,6 +103,7 @@ def lib():
         L.slim_block_fp8_untile.argtypes = [vp, i32, i32, vp, i64, vp]
         L.slim_block_fp8_gemm_workspace.argtypes = [i32, i32, i32, psz]
         L.slim_block_fp8_gemm.argtypes = [ctypes.POINTER(slim_block_fp8_layer), vp, vp, i32, vp, i64, i32, vp, sz, vp]
+        L.slim_block_fp8_gemm_plan.argtypes = [i32, i32, i32, i32, pi32]
         for name in EXPORTS[2:]:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -786,3 +788,11 @@ def slim_block_fp8_gemm(layer: SlimBlockFp8Weight, codes: torch.Tensor, scales: 
     if status != SLIM_OK:
         _check("slim_block_fp8_gemm", status)
     return Y
+
+
+def slim_block_fp8_gemm_plan(n: int, k: int, m: int, dtype: torch.dtype = torch.float16) -> dict:
+    """What slim_block_fp8_gemm would launch (host logic; no launch): kernel "stream" or "tile", rows and tokens of a workgroup's tile, its
+    threads, workgroups, and whether products are summed in binary32 (else by the 8-bit instruction)."""
+    out = (ctypes.c_int32 * 6)()
+    _check("slim_block_fp8_gemm_plan", lib().slim_block_fp8_gemm_plan(n, k, m, DTYPES[dtype], out))
+    return {"kernel": ("stream", "tile")[out[0]], "rows": out[1], "tokens": out[2], "threads": out[3], "workgroups": out[4], "binary32": bool(out[5])}

@@ -113,14 +113,17 @@ __device__ __forceinline__ void load_run_to_lds(rsrc_t r, uint32_t lane_off, uin
 // Bound by memory where the layer is large: 28672 x 8192 at 16 tokens 44 us, 5.3 TB/s, and 42 to 44 with the products left out.  Layers that fit the
 // last-level cache are bound by what a wavefront issues, conversions to fp16 first: 5120 x 5120 at 48 tokens 9.7 us on 160 of 256 compute units (more
 // workgroups of fewer fragments convert the tokens more often, the times are at launch_stream_of); 4096 x 4096 at one token 5.3 us, of which a launch is 3.
+constexpr int kStreamDepth = 2;             // blocks under way per wavefront
+
+constexpr size_t stream_lds(int fr, int tb, int waves)
+{
+    const size_t ring = (size_t)waves * (kStreamDepth * (fr + tb) * 2048 + 2048), sums = (size_t)waves * fr * tb * kWave * sizeof(float4_t);
+    return ring > sums ? ring : sums;
+}
+
 template <int FR, int TB>
 struct StreamLds {
     static constexpr int stage = (FR + TB) * 2048, scales = 2048;         // per wavefront: of a block; of twice four blocks
-    static constexpr size_t bytes(int waves, int depth)
-    {
-        const size_t ring = (size_t)waves * (depth * stage + scales), sums = (size_t)waves * FR * TB * kWave * sizeof(float4_t);
-        return ring > sums ? ring : sums;
-    }
 };
 
 template <int FR, int TB, int D, int THREADS, class T>
@@ -502,55 +505,52 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void block_tile_kernel(BlockG
     }
 }
 
-// S wavefronts, two blocks under way each: more of either was slower from 4096 rows on (28672 x 8192 at one token: 41 us with 4 or 8
-// wavefronts of one fragment, 52 with 16; three or four blocks under way 44 to 50).
-template <int FR, int TB, class T>
-static void launch_stream(const BlockGemmArgs &a, int waves, hipStream_t st)
-{
-    constexpr int D = 2, THREADS = 8 * kWave;
-    while (waves > 1 && StreamLds<FR, TB>::bytes(waves, D) > device_info().lds) waves /= 2;
-    if (waves > a.kb) waves = a.kb;
-    const size_t lds = StreamLds<FR, TB>::bytes(waves, D);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(block_stream_kernel<FR, TB, D, THREADS, T>), dim3((unsigned)(wtile_rows(a.n) * 4 / FR)),
-                       dim3((unsigned)(waves * kWave)), lds, st, a);
-}
-
-// As many fragments per workgroup as leave 160 workgroups: the tokens are read once per workgroup, and four fragments are a whole tile of weights.
-// us with one / two / four fragments: 28672 x 8192 at 16 tokens 49 / 51 / 45, at 64 tokens 96 / 72 / 58; 8192 x 8192 at 64 tokens 23 / 19 / 22;
+// As many fragments per workgroup as leave 160 workgroups for 256 compute units: the tokens are read once per workgroup, and four fragments are a whole tile
+// of weights.  us with one / two / four fragments: 28672 x 8192 at 16 tokens 49 / 51 / 45, at 64 tokens 96 / 72 / 58; 8192 x 8192 at 64 tokens 23 / 19 / 22;
 // 5120 x 5120 at 48 tokens 11.9 / 9.9 / 13.8; 4096 x 4096 at 32 tokens 6.9 / 7.3 / 9.2.  Two fragments are not worth it for up to 16 tokens
 // (8192 x 8192: 12.2 / 15.1 / 13.0).
+// Four wavefronts, two blocks under way each: more of either was slower for 28672 x 8192 at one token (41 us with 4 or 8 wavefronts of one
+// fragment, 52 with 16; three or four blocks under way 44 to 50).  Eight where there are fewer workgroups than compute units.
+struct StreamPlan {
+    int fragments, waves, workgroups;
+};
+static StreamPlan plan_stream(int n, int kb, int tb)
+{
+    const DeviceInfo dev = device_info();
+    const int all = wtile_rows(n) * 4, enough = dev.cus * 5 / 8;
+    StreamPlan p;
+    p.fragments = all >= 4 * enough ? 4 : tb > 1 && all >= 2 * enough ? 2 : 1;
+    p.waves = p.fragments == 1 && all < dev.cus ? 8 : 4;
+    while (p.waves > 1 && stream_lds(p.fragments, tb, p.waves) > dev.lds) p.waves /= 2;
+    if (p.waves > kb) p.waves = kb;
+    p.workgroups = all / p.fragments;
+    return p;
+}
+
+template <int FR, int TB, class T>
+static void launch_stream(const BlockGemmArgs &a, const StreamPlan &p, hipStream_t st)
+{
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(block_stream_kernel<FR, TB, kStreamDepth, 8 * kWave, T>), dim3((unsigned)p.workgroups),
+                       dim3((unsigned)(p.waves * kWave)), stream_lds(FR, TB, p.waves), st, a);
+}
+
 template <int TB, class T>
 static void launch_stream_of(const BlockGemmArgs &a, hipStream_t st)
 {
-    const int fragments = wtile_rows(a.n) * 4;
-    if (fragments >= 4 * 160) {
-        launch_stream<4, TB, T>(a, 4, st);
+    const StreamPlan p = plan_stream(a.n, a.kb, TB);
+    if (p.fragments == 4) {
+        launch_stream<4, TB, T>(a, p, st);
         return;
     }
     if constexpr (TB > 1)
-        if (fragments >= 2 * 160) {
-            launch_stream<2, TB, T>(a, 4, st);
+        if (p.fragments == 2) {
+            launch_stream<2, TB, T>(a, p, st);
             return;
         }
-    launch_stream<1, TB, T>(a, fragments < 256 ? 8 : 4, st);
+    launch_stream<1, TB, T>(a, p, st);
 }
 
-template <int KG, int WR, int WT, int AF, int BF, int STAGES, bool EXACT, class T>
-static int launch_tile(BlockGemmArgs a, hipStream_t st)
-{
-    constexpr int BM = 16 * AF * WR, BN = 16 * BF * WT;
-    constexpr size_t LDS = (size_t)KG * TileLds<BM, BN, STAGES>::bytes;
-    static_assert(KG <= 2 && LDS <= 160 * 1024 && (KG == 1 || (size_t)BM * BN * 4 <= LDS), "LDS");
-    a.tiles_o = (int)(((int64_t)a.n + BM - 1) / BM);
-    a.tiles_t = (int)(((int64_t)a.m + BN - 1) / BN);
-    const int64_t tiles = (int64_t)a.tiles_o * a.tiles_t;
-    if (tiles * (KG * WR * WT * kWave) > UINT32_MAX) return SLIM_ERR_SHAPE;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(block_tile_kernel<KG, WR, WT, AF, BF, STAGES, EXACT, T>), dim3((unsigned)tiles), dim3(KG * WR * WT * kWave), LDS,
-                       st, a);
-    return SLIM_OK;
-}
-
-// Tiles of block_tile_kernel: rows, tokens, workgroups per compute unit (by LDS), and the time per block of 128 inputs with every compute unit
+// Tiles of block_tile_kernel: rows, tokens, threads, workgroups per compute unit (by LDS), and the time per block of 128 inputs with every compute unit
 // at work and with at most half of them (less power, less traffic).  The times (us) are those of one to three rounds on 128 to
 // 4096 tokens, 4096 to 28672 rows and 4096 to 11008 inputs; a call takes rounds * (blocks * time + 3) or so, and the tile with the least of that
 // is taken.  us so, with the tiles in their order (the one taken in brackets):
@@ -563,16 +563,33 @@ static int launch_tile(BlockGemmArgs a, hipStream_t st)
 //   1024 tokens, 11008 x 4096   [46] 60  60  83  78  97
 // The smaller tiles are bound by the instructions a wavefront issues per block (its 32 additions per 8 products first of all), 256 x 256 by power.
 struct TileShape {
-    int rows, toks, per_cu;
+    int rows, toks, threads, per_cu;
     float full, half;
 };
-constexpr TileShape kTiles[] = {{256, 256, 1, 1.7f, 1.3f},   {256, 128, 1, 1.0f, 0.8f},  {128, 128, 1, 0.62f, 0.5f},
-                                {64, 128, 1, 0.40f, 0.38f}, {64, 64, 2, 0.45f, 0.33f}, {64, 64, 1, 0.24f, 0.24f}};
+constexpr TileShape kTiles[] = {{256, 256, 512, 1, 1.7f, 1.3f},   {256, 128, 512, 1, 1.0f, 0.8f},  {128, 128, 512, 1, 0.62f, 0.5f},
+                                {64, 128, 256, 1, 0.40f, 0.38f}, {64, 64, 256, 2, 0.45f, 0.33f}, {64, 64, 512, 1, 0.24f, 0.24f}};
 // (with results in fp32: 128 x 128, the same by two groups, 64 x 128 and 64 x 64 by two groups; 128 tokens on 4096 x 4096: 37, 31, 23, [16]; 256 tokens on
 // 5120 x 5120: 45, 37, [28], 35; 333 tokens on 10007 x 4100: 40, [36], 48, 61; 1024 tokens on 11008 x 4096: [87], 94, 131, 154)
-constexpr TileShape kExactTiles[] = {{128, 128, 2, 1.31f, 1.1f}, {128, 128, 1, 0.97f, 0.92f}, {64, 128, 1, 0.64f, 0.64f}, {64, 64, 1, 0.42f, 0.42f}};
+constexpr TileShape kExactTiles[] = {{128, 128, 256, 2, 1.31f, 1.1f}, {128, 128, 512, 1, 0.97f, 0.92f}, {64, 128, 512, 1, 0.64f, 0.64f}, {64, 64, 512, 1, 0.42f, 0.42f}};
 
-static int plan_tile(const BlockGemmArgs &a, bool exact)
+template <int SHAPE, int KG, int WR, int WT, int AF, int BF, int STAGES, bool EXACT, class T>
+static int launch_tile(BlockGemmArgs a, hipStream_t st)
+{
+    constexpr int BM = 16 * AF * WR, BN = 16 * BF * WT;
+    constexpr size_t LDS = (size_t)KG * TileLds<BM, BN, STAGES>::bytes;
+    constexpr TileShape shape = EXACT ? kExactTiles[SHAPE] : kTiles[SHAPE];
+    static_assert(shape.rows == BM && shape.toks == BN && shape.threads == KG * WR * WT * kWave && shape.per_cu * LDS <= 160 * 1024, "the table's tile");
+    static_assert(KG <= 2 && LDS <= 160 * 1024 && (KG == 1 || (size_t)BM * BN * 4 <= LDS), "LDS");
+    a.tiles_o = (int)(((int64_t)a.n + BM - 1) / BM);
+    a.tiles_t = (int)(((int64_t)a.m + BN - 1) / BN);
+    const int64_t tiles = (int64_t)a.tiles_o * a.tiles_t;
+    if (tiles * (KG * WR * WT * kWave) > UINT32_MAX) return SLIM_ERR_SHAPE;
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(block_tile_kernel<KG, WR, WT, AF, BF, STAGES, EXACT, T>), dim3((unsigned)tiles), dim3(KG * WR * WT * kWave), LDS,
+                       st, a);
+    return SLIM_OK;
+}
+
+static int plan_tile(int n, int kb, int m, bool exact)
 {
     const TileShape *shapes = exact ? kExactTiles : kTiles;
     const int count = exact ? (int)(sizeof kExactTiles / sizeof kExactTiles[0]) : (int)(sizeof kTiles / sizeof kTiles[0]);
@@ -581,9 +598,9 @@ static int plan_tile(const BlockGemmArgs &a, bool exact)
     double least = 0;
     for (int i = 0; i < count; ++i) {
         const TileShape &t = shapes[i];
-        const double tiles = (double)(((int64_t)a.n + t.rows - 1) / t.rows) * (double)(((int64_t)a.m + t.toks - 1) / t.toks);
+        const double tiles = (double)(((int64_t)n + t.rows - 1) / t.rows) * (double)(((int64_t)m + t.toks - 1) / t.toks);
         const double rounds = __builtin_ceil(tiles / (cus * t.per_cu));
-        const double time = rounds * (a.kb * (2 * tiles <= cus * t.per_cu ? t.half : t.full) + 3.0);
+        const double time = rounds * (kb * (2 * tiles <= cus * t.per_cu ? t.half : t.full) + 3.0);
         if (i == 0 || time < least) {
             least = time;
             best = i;
@@ -603,22 +620,22 @@ static int launch_block_gemm(const BlockGemmArgs &a, hipStream_t st)
     default: break;
     }
     constexpr bool EXACT = sizeof(typename T::type) == 4;
-    const int shape = plan_tile(a, EXACT);
+    const int shape = plan_tile(a.n, a.kb, a.m, EXACT);
     if constexpr (EXACT) {
         switch (shape) {
-        case 0: return launch_tile<1, 2, 2, 4, 4, 2, true, T>(a, st);
-        case 1: return launch_tile<2, 2, 2, 4, 4, 2, true, T>(a, st);
-        case 2: return launch_tile<2, 1, 4, 4, 2, 2, true, T>(a, st);
-        default: return launch_tile<2, 1, 4, 4, 1, 4, true, T>(a, st);
+        case 0: return launch_tile<0, 1, 2, 2, 4, 4, 2, true, T>(a, st);
+        case 1: return launch_tile<1, 2, 2, 2, 4, 4, 2, true, T>(a, st);
+        case 2: return launch_tile<2, 2, 1, 4, 4, 2, 2, true, T>(a, st);
+        default: return launch_tile<3, 2, 1, 4, 4, 1, 4, true, T>(a, st);
         }
     } else {
         switch (shape) {
-        case 0: return launch_tile<1, 2, 4, 8, 4, 2, false, T>(a, st);
-        case 1: return launch_tile<1, 4, 2, 4, 4, 3, false, T>(a, st);
-        case 2: return launch_tile<1, 2, 4, 4, 2, 4, false, T>(a, st);
-        case 3: return launch_tile<1, 1, 4, 4, 2, 4, false, T>(a, st);
-        case 4: return launch_tile<1, 1, 4, 4, 1, 4, false, T>(a, st);
-        default: return launch_tile<2, 1, 4, 4, 1, 4, false, T>(a, st);
+        case 0: return launch_tile<0, 1, 2, 4, 8, 4, 2, false, T>(a, st);
+        case 1: return launch_tile<1, 1, 4, 2, 4, 4, 3, false, T>(a, st);
+        case 2: return launch_tile<2, 1, 2, 4, 4, 2, 4, false, T>(a, st);
+        case 3: return launch_tile<3, 1, 1, 4, 4, 2, 4, false, T>(a, st);
+        case 4: return launch_tile<4, 1, 1, 4, 4, 1, 4, false, T>(a, st);
+        default: return launch_tile<5, 2, 1, 4, 4, 1, 4, false, T>(a, st);
         }
     }
 }
@@ -632,6 +649,30 @@ extern "C" int slim_block_fp8_gemm_workspace(int32_t n, int32_t k, int32_t m, si
     if (!bytes) return SLIM_ERR_NULL;
     if (slim_block_fp8_weight_sizes(n, k, nullptr, nullptr) != SLIM_OK || m < 1) return SLIM_ERR_SHAPE;
     *bytes = 256;
+    return SLIM_OK;
+}
+
+// What slim_block_fp8_gemm would launch (no launch, no device access but for its number of compute units).
+extern "C" int slim_block_fp8_gemm_plan(int32_t n, int32_t k, int32_t m, int32_t dtype, int32_t *out)
+{
+    if (!out) return SLIM_ERR_NULL;
+    if (slim_block_fp8_weight_sizes(n, k, nullptr, nullptr) != SLIM_OK || m < 1 || (dtype != SLIM_F16 && dtype != SLIM_BF16 && dtype != SLIM_F32))
+        return SLIM_ERR_SHAPE;
+    const int kb = blocks_of(k);
+    if (m <= 64) {
+        const int tb = (m + 15) / 16;
+        const StreamPlan p = plan_stream(n, kb, tb);
+        const int32_t plan[6] = {0, 16 * p.fragments, 16 * tb, p.waves * kWave, p.workgroups, 1};
+        for (int i = 0; i < 6; ++i) out[i] = plan[i];
+        return SLIM_OK;
+    }
+    const bool exact = dtype == SLIM_F32;
+    const int shape = plan_tile(n, kb, m, exact);
+    const TileShape &t = exact ? kExactTiles[shape] : kTiles[shape];
+    const int64_t tiles = (((int64_t)n + t.rows - 1) / t.rows) * (((int64_t)m + t.toks - 1) / t.toks);
+    if (tiles * t.threads > UINT32_MAX) return SLIM_ERR_SHAPE;
+    const int32_t plan[6] = {1, t.rows, t.toks, t.threads, (int32_t)tiles, exact ? 1 : 0};
+    for (int i = 0; i < 6; ++i) out[i] = plan[i];
     return SLIM_OK;
 }
 
