@@ -719,8 +719,6 @@ class _LayerRef:
     layer: slim_block_fp8_layer
     address: int
     device: int
-    codes: tuple           # (address, elements)
-    scales: tuple
 
 
 @dataclass
@@ -731,21 +729,19 @@ class SlimBlockFp8Weight:
     codes: torch.Tensor            # uint8, in tiles (slim_block_fp8_weight, slim_block_fp8_tile)
     scales: torch.Tensor           # float32 [ceil(n / 128)][ceil(k / 128)]
 
-    def c_ref(self):
-        """What the product is given of the layer; the buffers are checked when it is made, once per layer and again after any field is
-        assigned or a tensor has other data."""
-        c, s = self.codes, self.scales
-        at = (c.data_ptr(), c.numel()), (s.data_ptr(), s.numel())
+    def c_ref(self, again: bool = False):
+        """What the product is given of the layer; the buffers are checked when it is made, once per layer, after any field is assigned, and where
+        `again` is set (the product asks for that where a tensor's data is not what it was)."""
         ref = self.__dict__.get("_ref")
-        if ref is None or (ref.codes, ref.scales) != at:
+        if ref is None or again:
             self.__dict__.pop("_ref", None)
             size = slim_block_fp8_weight_sizes(self.n, self.k)
-            _dev(c, torch.uint8, "codes")
-            _dev(s, torch.float32, "scales")
-            if c.numel() != size["codes"] or s.numel() * 4 != size["scales"] or s.device != c.device:
+            _dev(self.codes, torch.uint8, "codes")
+            _dev(self.scales, torch.float32, "scales")
+            if self.codes.numel() != size["codes"] or self.scales.numel() * 4 != size["scales"] or self.scales.device != self.codes.device:
                 raise ValueError("codes and scales are not an n x k layer's on one device")
-            cs = slim_block_fp8_layer(self.n, self.k, c.data_ptr(), s.data_ptr())
-            ref = _LayerRef(cs, ctypes.addressof(cs), c.get_device(), *at)
+            cs = slim_block_fp8_layer(self.n, self.k, self.codes.data_ptr(), self.scales.data_ptr())
+            ref = _LayerRef(cs, ctypes.addressof(cs), self.codes.get_device())
             self.__dict__["_ref"] = ref
         return ref
 
@@ -786,7 +782,10 @@ def slim_block_fp8_gemm(layer: SlimBlockFp8Weight, codes: torch.Tensor, scales: 
         Y = torch.empty(codes.shape[0], layer.n, dtype=dtype, device=layer.codes.device)
     if workspace is None:
         workspace = alloc_block_fp8_workspace(layer, codes.shape[0])
-    status = (_call or _calls()).gemm(ref.address, ref.device, codes, scales, Y, workspace)
+    status = (_call or _calls()).gemm(ref.address, ref.device, layer.codes, layer.scales, codes, scales, Y, workspace)
+    if status > 0:                                    # the layer's tensors have other data than the reference says
+        ref = layer.c_ref(again=True)
+        status = _call.gemm(ref.address, ref.device, layer.codes, layer.scales, codes, scales, Y, workspace)
     if status != SLIM_OK:
         _check("slim_block_fp8_gemm", status)
     return Y

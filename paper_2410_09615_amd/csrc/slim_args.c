@@ -178,28 +178,33 @@ static PyObject *act(PyObject *self, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(status);
 }
 
-/* gemm(layer's address, layer's device, codes, scales, Y, workspace) -> status */
+/* gemm(layer's address, layer's device, the layer's codes and scales, codes, scales, Y, workspace) -> status, or 1 (nothing enqueued) where the layer's
+   tensors are no longer where its struct says */
 static PyObject *gemm(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
     (void)self;
-    if (n != 6) return PyErr_Format(PyExc_TypeError, "gemm takes 6 arguments");
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "gemm takes 8 arguments");
     const slim_block_fp8_layer *layer = PyLong_AsVoidPtr(a[0]);
     const long long device = PyLong_AsLongLong(a[1]);
     if (PyErr_Occurred() || !layer) return refuse("layer", "has no address"), NULL;
     matrix c, y;
     void *scales, *st;
     int status;
-    const long long kb = ((long long)layer->k + 127) / 128;
-    if (rows(a[2], "codes", &c)) return NULL;
+    const long long kb = ((long long)layer->k + 127) / 128, row_tiles = ((long long)layer->n + 63) / 64;
+    const int stale = address(a[2]) != layer->codes || address(a[3]) != layer->scales || number(a[2], s_numel) != row_tiles * kb * 8192 ||
+                      number(a[3], s_numel) != (row_tiles + 1) / 2 * kb;
+    if (PyErr_Occurred()) return NULL;
+    if (stale) return PyLong_FromLong(1);
+    if (rows(a[4], "codes", &c)) return NULL;
     if ((c.type != U8 && c.type != E4M3) || c.device != device || c.k != kb * 128 || (c.m > 1 && c.ld != c.k))
         return refuse("codes", "must be contiguous uint8 [m][128 ceil(k / 128)] on the layer's device"), NULL;
-    if (whole(a[3], "scales", SLIM_F32, SLIM_F32, c.m * kb, device, &scales)) return NULL;
-    if (rows(a[4], "Y", &y)) return NULL;
+    if (whole(a[5], "scales", SLIM_F32, SLIM_F32, c.m * kb, device, &scales)) return NULL;
+    if (rows(a[6], "Y", &y)) return NULL;
     if (y.type > SLIM_F32 || y.device != device || y.m != c.m || y.k != layer->n)
         return refuse("Y", "must be a float16, bfloat16 or float32 matrix [m][n] on the layer's device"), NULL;
-    const long long room = number(a[5], s_numel);
+    const long long room = number(a[7], s_numel);
     void *ws;
-    if (room < 0 || whole(a[5], "workspace", U8, U8, room, device, &ws) || stream(device, &st)) return NULL;
+    if (room < 0 || whole(a[7], "workspace", U8, U8, room, device, &ws) || stream(device, &st)) return NULL;
     Py_BEGIN_ALLOW_THREADS
     status = call_gemm(layer, c.p, scales, (int32_t)c.m, y.p, y.ld, y.type, ws, (size_t)room, st);
     Py_END_ALLOW_THREADS
