@@ -9,7 +9,8 @@
 // is more than 13 bits below it (measured with single products; between pieces, and in the 16-bit instruction, nothing above 2^-23 is lost).
 // On blocks as they are quantized here that is 1.5e-5 to 8e-5 of a result (2-norm), below the 2.1e-4 of its rounding to fp16
 // and far below what 8-bit codes carry; results in fp32 are asked for to be better than that, and the 16-bit instructions are
-// half as fast.  So results in fp32 are EXACT, as is the kernel for few tokens, which waits for memory either way.
+// half as fast.  So results in fp32 are EXACT, as is the kernel for few tokens: for layers larger than the last-level cache, where it waits for memory, that
+// costs nothing; on smaller ones the conversions to fp16 are what bounds it (block_stream_kernel).
 #include <hip/hip_runtime.h>
 
 #include "slim_block_fp8.h"
@@ -561,7 +562,8 @@ static void launch_stream_of(const BlockGemmArgs &a, hipStream_t st)
 //   700 tokens, 4096 x 4096      43  28 [19] 29  25  28
 //   1000 tokens, 8192 x 8192     80 [63] 77 105 108 125
 //   1024 tokens, 11008 x 4096   [46] 60  60  83  78  97
-// The smaller tiles are bound by the instructions a wavefront issues per block (its 32 additions per 8 products first of all), 256 x 256 by power.
+// 256 x 256 is bound by power.  What bounds the smaller tiles was not measured: a block of 64 x 128 takes 0.40 us, 960 cycles, of which a wavefront's 8 products
+// and 32 additions are under 400, and its 24.6 KB arrive at 61 GB/s per compute unit (64 x 64: 68, 128 x 128: 53).
 struct TileShape {
     int rows, toks, threads, per_cu;
     float full, half;
