@@ -279,6 +279,8 @@ int slim_unpack(const uint8_t *qvals, const uint8_t *meta, slim_shape shape, int
  * Scratch the forward calls need for a layer at m tokens (a HOST out-pointer).
  * The same size covers slim_linear_gemv (m <= 16), slim_linear_gemm and
  * slim_lowrank.
+ * It does not grow with m throughout: T = X R^T of fewer tokens may be split into
+ * more ranges, and decode calls have partial sums of their own.
  * The workspace must be ZERO-FILLED ONCE before its first use (hipMemset):
  * its first bytes hold the decode path's T = X R^T between the kernels' two
  * phases (pieces tagged with a call number, never 0), and a fresh workspace
