@@ -586,6 +586,73 @@ int slim_block_fp8_gemm(const slim_block_fp8_layer *layer, const uint8_t *X, con
 int slim_block_fp8_gemm_plan(int32_t n, int32_t k, int32_t m, int32_t dtype, int32_t *out);
 
 /*
+ * 4-bit layers with a scale for each group of inputs, dense (no 2:4 mask): the form in which most 4-bit checkpoints hold their weights, and the one that
+ * the paper's kernels for a single scale are compared with (group 128, Table 17).  Of a group of 32, 64 or 128 inputs of a row (a row's last group may be
+ * shorter), codes c of 4 bits, a scale s (fp16) and a zero point z (0 .. 15; symmetric weights have 8 throughout and keep none):
+ *   value = (c - z) s;
+ *   symmetric:         s = fp16(max |w| / 7),       c = clamp(rint(w / s), -8, 7) + 8;
+ *   with zero points:  s = fp16((hi - lo) / 15),    z = clamp(rint(-lo / s), 0, 15),   c = clamp(rint(w / s) + z, 0, 15),
+ *                      lo = the smallest of the weights and 0, hi = the largest of them and 0;
+ * differences, quotients and rint (ties to even) in binary32, s 1 for a group of zeros, the smallest positive fp16 where it would round to 0, at most 65504.
+ * A group that holds an infinity or a NaN has a NaN for its scale.
+ *   codes   blocks of 16 rows x 128 inputs (1 KiB), row block major, ceil(k / 128) blocks per row block, rows and inputs padded with zero codes.
+ *           Row r, input 32 j + 8 q + 2 i + h of a block (i 0 .. 3, h 0 or 1) is nibble i + 4 h (bits 4 (i + 4 h) ..) of the dword at (16 q + r) 16 + 4 j;
+ *   scales  fp16 [n][ceil(k / group)] and zeros uint8 of the same shape, row-major: as a checkpoint has them (slim_group_q4_sizes).
+ * Scales that are not finite make the results that they are part of not finite; a zero point may be any byte.
+ * Matrices of inputs and results may have any alignment of whole elements and a row stride (`_ld`, in elements, at least the row's length); codes are
+ * 16-byte aligned.  k <= 2^22.  No call has a workspace, and none keeps anything.  Results do not depend on the order of workgroups.  All enqueue kernels
+ * only and may be captured into a HIP graph.
+ */
+typedef struct {
+    int32_t n, k, group;
+    const uint8_t *codes;
+    const slim_half *scales;
+    const uint8_t *zeros;   /* NULL: symmetric */
+} slim_group_q4_layer;
+
+/* Sizes in bytes (HOST out-pointers, NULL individually).  Errors: SHAPE (n, k < 1, k > 2^22, group not 32, 64 or 128). */
+int slim_group_q4_sizes(int32_t n, int32_t k, int32_t group, size_t *codes_bytes, size_t *scales_bytes, size_t *zeros_bytes);
+
+/*
+ * slim_group_q4_weight -- W [n][k] of any slim_dtype to codes, scales and (where `zeros` is given) zero points.
+ * slim_group_q4_tile   -- row-major codes, a byte each (its low four bits; row stride ld bytes), to the blocks, for codes that a checkpoint brings;
+ * slim_group_q4_untile is its inverse.
+ * slim_group_q4_values -- what a layer's codes stand for, [n][k] rounded once to any slim_dtype.
+ * Errors: NULL, SHAPE, ALIGN, HIP.
+ */
+int slim_group_q4_weight(const void *W, int64_t ld, int32_t dtype, int32_t n, int32_t k, int32_t group, uint8_t *codes, slim_half *scales, uint8_t *zeros,
+                         void *stream);
+int slim_group_q4_tile(const uint8_t *in, int64_t ld, int32_t n, int32_t k, uint8_t *codes, void *stream);
+int slim_group_q4_untile(const uint8_t *codes, int32_t n, int32_t k, uint8_t *out, int64_t ld, void *stream);
+int slim_group_q4_values(const slim_group_q4_layer *layer, void *out, int64_t ld, int32_t dtype, void *stream);
+
+/*
+ * slim_group_q4_gemm   -- Y = X W^T:  X [m][k], Y [m][n] of `dtype` (SLIM_F16, SLIM_BF16), any m >= 1.
+ * slim_group_q4_gemm_t -- dX = dY W:  the gradient of X through frozen weights; dY [m][n], dX [m][k].
+ * Sums in binary32, one rounding of each result.
+ * X, Y (dY, dX) do not overlap.  Errors: NULL, SHAPE, ALIGN, HIP.
+ */
+int slim_group_q4_gemm(const slim_group_q4_layer *layer, const void *X, int64_t x_ld, int32_t m, void *Y, int64_t y_ld, int32_t dtype, void *stream);
+int slim_group_q4_gemm_t(const slim_group_q4_layer *layer, const void *dY, int64_t dy_ld, int32_t m, void *dX, int64_t dx_ld, int32_t dtype, void *stream);
+
+/*
+ * slim_group_q4_gated -- the first half of a gated feed-forward block in one kernel:
+ *   G = X Wg^T,  U = X Wu^T,  H = silu(G) * U  (silu(g) = g / (1 + exp(-g))),
+ * gate and up of one n, k and group (each with zero points or without); G and U in binary32 inside.  H [m][n]; G and U, where they are given, receive
+ * them rounded: what the backward call wants.
+ * slim_group_q4_gated_backward -- gradients through the block, its weights frozen:
+ *   dU = dH silu(G),  dG = dH U sigma(G) (1 + G (1 - sigma(G))),  dX = dG Wg + dU Wu,
+ * all of `dtype`; dG and dU [m][n] (what a low-rank term beside the layers needs) are rounded once, and dX is the product of the rounded ones.
+ * dG may be G or dH, dU may be U or dH (same pointer and stride), not both the same; no other overlap.
+ * Errors: NULL, SHAPE (the two layers' sizes too), ALIGN, HIP.
+ */
+int slim_group_q4_gated(const slim_group_q4_layer *gate, const slim_group_q4_layer *up, const void *X, int64_t x_ld, int32_t m, void *H, int64_t h_ld, void *G,
+                        int64_t g_ld, void *U, int64_t u_ld, int32_t dtype, void *stream);
+int slim_group_q4_gated_backward(const slim_group_q4_layer *gate, const slim_group_q4_layer *up, const void *dH, int64_t dh_ld, const void *G, int64_t g_ld,
+                                 const void *U, int64_t u_ld, int32_t m, void *dG, int64_t dg_ld, void *dU, int64_t du_ld, void *dX, int64_t dx_ld,
+                                 int32_t dtype, void *stream);
+
+/*
  * Measurement aids (they compute nothing of the method): what this machine
  * delivers on a plain streaming read and on back-to-back matrix instructions,
  * to set beside the nominal peaks when a kernel's roofline fraction is quoted

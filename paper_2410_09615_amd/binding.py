@@ -38,6 +38,11 @@ class slim_block_fp8_layer(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int32), ("k", ctypes.c_int32), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
 
 
+class slim_group_q4_layer(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("k", ctypes.c_int32), ("group", ctypes.c_int32), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("zeros", ctypes.c_void_p)]
+
+
 SLIM_OK, SLIM_ERR_NULL, SLIM_ERR_SHAPE, SLIM_ERR_ALIGN, SLIM_ERR_WORKSPACE, SLIM_ERR_HIP, SLIM_ERR_WAIT = 0, -1, -2, -3, -4, -5, -6
 
 EXPORTS = ["slim_status_string", "slim_rank_pad", "slim_packed_sizes", "slim_pack", "slim_pack_adapters",
@@ -49,7 +54,9 @@ EXPORTS = ["slim_status_string", "slim_rank_pad", "slim_packed_sizes", "slim_pac
            "slim_linear_gemm_fp8",
            "slim_block_fp8_sizes", "slim_block_fp8_weight_sizes", "slim_block_fp8_norm", "slim_block_fp8_act", "slim_block_fp8_weight",
            "slim_block_fp8_tile", "slim_block_fp8_untile", "slim_block_fp8_gemm_workspace", "slim_block_fp8_gemm",
-           "slim_block_fp8_gemm_plan"]
+           "slim_block_fp8_gemm_plan",
+           "slim_group_q4_sizes", "slim_group_q4_weight", "slim_group_q4_tile", "slim_group_q4_untile", "slim_group_q4_values", "slim_group_q4_gemm",
+           "slim_group_q4_gemm_t", "slim_group_q4_gated", "slim_group_q4_gated_backward"]
 
 
 def lib():
@@ -104,6 +111,15 @@ def lib():
         L.slim_block_fp8_gemm_workspace.argtypes = [i32, i32, i32, psz]
         L.slim_block_fp8_gemm.argtypes = [ctypes.POINTER(slim_block_fp8_layer), vp, vp, i32, vp, i64, i32, vp, sz, vp]
         L.slim_block_fp8_gemm_plan.argtypes = [i32, i32, i32, i32, pi32]
+        pq4 = ctypes.POINTER(slim_group_q4_layer)
+        L.slim_group_q4_sizes.argtypes = [i32, i32, i32, psz, psz, psz]
+        L.slim_group_q4_weight.argtypes = [vp, i64, i32, i32, i32, i32, vp, vp, vp, vp]
+        L.slim_group_q4_tile.argtypes = [vp, i64, i32, i32, vp, vp]
+        L.slim_group_q4_untile.argtypes = [vp, i32, i32, vp, i64, vp]
+        L.slim_group_q4_values.argtypes = [pq4, vp, i64, i32, vp]
+        L.slim_group_q4_gemm.argtypes = L.slim_group_q4_gemm_t.argtypes = [pq4, vp, i64, i32, vp, i64, i32, vp]
+        L.slim_group_q4_gated.argtypes = [pq4, pq4, vp, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp]
+        L.slim_group_q4_gated_backward.argtypes = [pq4, pq4, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp]
         for name in EXPORTS[2:]:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -592,7 +608,7 @@ _call = None
 
 
 def _calls():
-    """The block operators' calls with their arguments looked at in C (csrc/slim_args.c), made ready once."""
+    """The block and group operators' calls with their arguments looked at in C (csrc/slim_args.c), made ready once."""
     global _call
     if _call is None:
         L = lib()
@@ -602,8 +618,9 @@ def _calls():
             raise RuntimeError("the _slim_args extension is missing: build it with `python -m paper_2410_09615_amd.build` "
                                "(there is no fallback path)") from e
         entry = lambda f: ctypes.cast(f, ctypes.c_void_p).value
-        _slim_args.init((torch.float16, torch.bfloat16, torch.float32, torch.uint8, _E4M3), torch._C._cuda_getCurrentRawStream,
-                        entry(L.slim_block_fp8_norm), entry(L.slim_block_fp8_act), entry(L.slim_block_fp8_gemm))
+        _slim_args.init((torch.float16, torch.bfloat16, torch.float32, torch.uint8, _E4M3), torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice,
+                        entry(L.slim_block_fp8_norm), entry(L.slim_block_fp8_act), entry(L.slim_block_fp8_gemm), entry(L.slim_group_q4_gemm),
+                        entry(L.slim_group_q4_gemm_t), entry(L.slim_group_q4_gated), entry(L.slim_group_q4_gated_backward))
         _call = _slim_args
     return _call
 
@@ -797,3 +814,189 @@ def slim_block_fp8_gemm_plan(n: int, k: int, m: int, dtype: torch.dtype = torch.
     out = (ctypes.c_int32 * 6)()
     _check("slim_block_fp8_gemm_plan", lib().slim_block_fp8_gemm_plan(n, k, m, DTYPES[dtype], out))
     return {"kernel": ("stream", "tile")[out[0]], "rows": out[1], "tokens": out[2], "threads": out[3], "workgroups": out[4], "binary32": bool(out[5])}
+
+
+# ---- 4-bit layers with a scale for each group of inputs ----
+def slim_group_q4_sizes(n: int, k: int, group: int = 128) -> dict:
+    c, s, z = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
+    _check("slim_group_q4_sizes", lib().slim_group_q4_sizes(n, k, group, c, s, z))
+    return {"codes": c.value, "scales": s.value, "zeros": z.value}
+
+
+@dataclass
+class SlimGroupQ4Weight:
+    """Device buffers of one layer of 4-bit weights with a scale per group (what `slim_group_q4_layer` points at)."""
+    n: int
+    k: int
+    group: int                     # inputs to a scale: 32, 64 or 128
+    codes: torch.Tensor            # uint8, in blocks (slim_group_q4_weight, slim_group_q4_tile)
+    scales: torch.Tensor           # float16 [n][ceil(k / group)]
+    zeros: torch.Tensor | None = None    # uint8 of the same shape, or None: symmetric
+
+    def c_ref(self, again: bool = False):
+        """What the calls are given of the layer; the buffers are checked when it is made, once per layer, after any field is assigned, and where
+        `again` is set (the calls ask for that where a tensor's data is not what it was)."""
+        ref = self.__dict__.get("_ref")
+        if ref is None or again:
+            self.__dict__.pop("_ref", None)
+            size = slim_group_q4_sizes(self.n, self.k, self.group)
+            _dev(self.codes, torch.uint8, "codes")
+            _dev(self.scales, torch.float16, "scales")
+            if self.codes.numel() != size["codes"] or self.scales.numel() * 2 != size["scales"] or self.scales.device != self.codes.device:
+                raise ValueError("codes and scales are not an n x k layer's on one device")
+            if self.zeros is not None:
+                _dev(self.zeros, torch.uint8, "zeros")
+                if self.zeros.numel() != size["zeros"] or self.zeros.device != self.codes.device:
+                    raise ValueError("zeros are not an n x k layer's on its device")
+            cs = slim_group_q4_layer(self.n, self.k, self.group, self.codes.data_ptr(), self.scales.data_ptr(),
+                                     None if self.zeros is None else self.zeros.data_ptr())
+            ref = _LayerRef(cs, ctypes.addressof(cs), self.codes.get_device())
+            self.__dict__["_ref"] = ref
+        return ref
+
+    def __setattr__(self, name, value):
+        self.__dict__.pop("_ref", None)
+        object.__setattr__(self, name, value)
+
+    def __getstate__(self):
+        """The fields: a copy or a stored layer has buffers of its own, and makes its own reference to them."""
+        return {name: value for name, value in self.__dict__.items() if name != "_ref"}
+
+
+def alloc_group_q4(n: int, k: int, group: int = 128, zeros: bool = False, device="cuda") -> SlimGroupQ4Weight:
+    """A layer's buffers, not filled: what slim_group_q4_weight writes."""
+    size, kg = slim_group_q4_sizes(n, k, group), (k + group - 1) // group
+    return SlimGroupQ4Weight(n, k, group, torch.empty(size["codes"], dtype=torch.uint8, device=device),
+                             torch.empty(n, kg, dtype=torch.float16, device=device),
+                             torch.empty(n, kg, dtype=torch.uint8, device=device) if zeros else None)
+
+
+def _on_device(device: int, call):
+    """call() with the device current."""
+    if torch.cuda.current_device() == device:
+        return call()
+    with torch.cuda.device(device):
+        return call()
+
+
+def slim_group_q4_weight(W: torch.Tensor, group: int = 128, zeros: bool = False, layer: SlimGroupQ4Weight | None = None) -> SlimGroupQ4Weight:
+    """W [n][k] fp32, fp16 or bf16 (any row stride) in 4 bits with a scale, and with `zeros` a zero point, per `group` inputs; or into the buffers
+    of `layer` (its group; zero points if it has them)."""
+    if W.dtype not in DTYPES:
+        raise ValueError("W must be float32, float16 or bfloat16")
+    ld = _rows(W, "W", W.dtype, None, W.get_device())
+    n, k = W.shape
+    if layer is None:
+        layer = alloc_group_q4(n, k, group, zeros, W.device)
+    ref = layer.c_ref(again=True)
+    if (layer.n, layer.k) != (n, k) or ref.device != W.get_device():
+        raise ValueError("layer must be of W's size, on its device")
+    c = ref.layer
+    _check("slim_group_q4_weight", _on_device(ref.device, lambda: lib().slim_group_q4_weight(_ptr(W), ld, DTYPES[W.dtype], n, k, layer.group, c.codes, c.scales,
+                                                                                           c.zeros, _stream(W))))
+    return layer
+
+
+def compress_group_q4(W: torch.Tensor, group: int = 128, zeros: bool = False) -> SlimGroupQ4Weight:
+    """slim_group_q4_weight into a new layer."""
+    return slim_group_q4_weight(W, group, zeros)
+
+
+def slim_group_q4_tile(codes: torch.Tensor) -> torch.Tensor:
+    """Row-major codes uint8 [n][k], a byte each (any row stride) -> uint8 in blocks, flat."""
+    ld = _rows(codes, "codes", torch.uint8, None, codes.get_device())
+    n, k = codes.shape
+    out = torch.empty(slim_group_q4_sizes(n, k)["codes"], dtype=torch.uint8, device=codes.device)
+    _check("slim_group_q4_tile", _on_device(codes.get_device(), lambda: lib().slim_group_q4_tile(_ptr(codes), ld, n, k, _ptr(out), _stream(codes))))
+    return out
+
+
+def slim_group_q4_untile(codes: torch.Tensor, n: int, k: int) -> torch.Tensor:
+    """Inverse of slim_group_q4_tile: uint8 [n][k]."""
+    _dev(codes, torch.uint8, "codes")
+    if codes.numel() != slim_group_q4_sizes(n, k)["codes"]:
+        raise ValueError("codes are not an n x k layer's")
+    out = torch.empty(n, k, dtype=torch.uint8, device=codes.device)
+    _check("slim_group_q4_untile", _on_device(codes.get_device(), lambda: lib().slim_group_q4_untile(_ptr(codes), n, k, _ptr(out), k, _stream(codes))))
+    return out
+
+
+def slim_group_q4_values(layer: SlimGroupQ4Weight, dtype: torch.dtype = torch.float16, values: torch.Tensor | None = None) -> torch.Tensor:
+    """What the layer's codes stand for: [n][k] of `dtype`, or into `values` (fp32, fp16 or bf16, any row stride)."""
+    ref = layer.c_ref(again=True)
+    if values is None:
+        if dtype not in DTYPES:
+            raise ValueError("dtype is float16, bfloat16 or float32")
+        values = torch.empty(layer.n, layer.k, dtype=dtype, device=layer.codes.device)
+    if values.dtype not in DTYPES:
+        raise ValueError("values must be float32, float16 or bfloat16")
+    ld = _rows(values, "values", values.dtype, (layer.n, layer.k), ref.device)
+    _check("slim_group_q4_values", _on_device(ref.device, lambda: lib().slim_group_q4_values(ref.layer, _ptr(values), ld, DTYPES[values.dtype], _stream(values))))
+    return values
+
+
+def _q4_call(name: str, device: int, call):
+    """call(again) until it has been enqueued: once more with the layers' references made anew, or with the tensors' device current."""
+    status = call(False)
+    if status == 1:                                   # a layer's tensors have other data than its reference says
+        status = call(True)
+    if status == 2:                                   # another device is current
+        with torch.cuda.device(device):
+            status = call(False)
+    if status != SLIM_OK:
+        _check(name, status)
+
+
+def _q4_product(name: str, transposed: bool, layer: SlimGroupQ4Weight, X: torch.Tensor, Y) -> torch.Tensor:
+    ref = layer.c_ref()
+    if Y is None:
+        Y = torch.empty(X.shape[0], layer.k if transposed else layer.n, dtype=X.dtype, device=layer.codes.device)
+    status = (_call or _calls()).q4_product(transposed, ref.address, ref.device, layer.codes, layer.scales, layer.zeros, X, Y)
+    if status != SLIM_OK:
+        def call(again):
+            r = layer.c_ref(again)
+            return _call.q4_product(transposed, r.address, r.device, layer.codes, layer.scales, layer.zeros, X, Y)
+        _q4_call(name, ref.device, call)
+    return Y
+
+
+def slim_group_q4_gemm(layer: SlimGroupQ4Weight, X: torch.Tensor, Y=None) -> torch.Tensor:
+    """Y [m][n] = X W^T; X fp16 or bf16 [m][k], Y of its type (None: a new one), any row strides, any m >= 1."""
+    return _q4_product("slim_group_q4_gemm", False, layer, X, Y)
+
+
+def slim_group_q4_gemm_t(layer: SlimGroupQ4Weight, dY: torch.Tensor, dX=None) -> torch.Tensor:
+    """dX [m][k] = dY W: the gradient of the product's input (the weights are frozen); dY fp16 or bf16 [m][n], dX of its type."""
+    return _q4_product("slim_group_q4_gemm_t", True, layer, dY, dX)
+
+
+def _q4_pair(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight, again: bool):
+    g, u = gate.c_ref(again), up.c_ref(again)
+    return g.address, g.device, gate.codes, gate.scales, gate.zeros, u.address, u.device, up.codes, up.scales, up.zeros
+
+
+def slim_group_q4_gated(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight, X: torch.Tensor, H=None, G=None, U=None):
+    """H [m][n] = silu(X Wg^T) * (X Wu^T) -> (H, G, U).  G, U: True for a new matrix that receives the two products (what
+    slim_group_q4_gated_backward wants), or one to write; None (returned as such): not wanted.  All of X's type, any row strides, any m >= 1."""
+    ref = gate.c_ref()
+    if H is None or G is True or U is True:
+        new = lambda: torch.empty(X.shape[0], gate.n, dtype=X.dtype, device=gate.codes.device)
+        H, G, U = new() if H is None else H, new() if G is True else G, new() if U is True else U
+    status = (_call or _calls()).q4_gated(*_q4_pair(gate, up, False), X, H, G, U)
+    if status != SLIM_OK:
+        _q4_call("slim_group_q4_gated", ref.device, lambda again: _call.q4_gated(*_q4_pair(gate, up, again), X, H, G, U))
+    return H, G, U
+
+
+def slim_group_q4_gated_backward(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight, dH: torch.Tensor, G: torch.Tensor, U: torch.Tensor, dG=None, dU=None,
+                                 dX=None):
+    """Gradients through slim_group_q4_gated, its weights frozen: dH, G, U [m][n] -> (dX [m][k], dG [m][n], dU [m][n]), all of one type.
+    dG may be G or dH and dU may be U or dH, but not both the same."""
+    ref = gate.c_ref()
+    if dG is None or dU is None or dX is None:
+        new = lambda k: torch.empty(dH.shape[0], k, dtype=dH.dtype, device=gate.codes.device)
+        dG, dU, dX = new(gate.n) if dG is None else dG, new(gate.n) if dU is None else dU, new(gate.k) if dX is None else dX
+    status = (_call or _calls()).q4_backward(*_q4_pair(gate, up, False), dH, G, U, dG, dU, dX)
+    if status != SLIM_OK:
+        _q4_call("slim_group_q4_gated_backward", ref.device, lambda again: _call.q4_backward(*_q4_pair(gate, up, again), dH, G, U, dG, dU, dX))
+    return dX, dG, dU

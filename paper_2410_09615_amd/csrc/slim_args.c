@@ -1,4 +1,4 @@
-/* Argument marshalling of the block operators for the Python binding.
+/* Argument marshalling of the block and group operators for the Python binding.
  *
  * A call on one token runs for 3 to 6 us on the GPU and takes 3 us to launch; looking at six tensors from Python took 4 us more.
  * Here each is looked at once: its type, device, shape and strides, and its address, through the methods that tensors have
@@ -14,12 +14,19 @@
 static PyObject *s_dtype, *s_shape, *s_stride, *s_get_device, *s_data_ptr, *s_numel, *s_is_contiguous;
 static PyObject *types[5];               /* fp16, bf16, fp32 (slim_dtype's numbers), uint8, E4M3 */
 enum { U8 = 3, E4M3 = 4 };
-static PyObject *stream_of;
+static PyObject *stream_of, *device_now;
 static int (*call_norm)(const void *, int64_t, const void *, int64_t, const void *, int32_t, int32_t, int32_t, int32_t, float, void *,
                         int64_t, void *, int64_t, uint8_t *, float *, void *);
 static int (*call_act)(const void *, int64_t, const void *, int64_t, int32_t, int32_t, int32_t, int32_t, uint8_t *, float *, void *);
 static int (*call_gemm)(const slim_block_fp8_layer *, const uint8_t *, const float *, int32_t, void *, int64_t, int32_t, void *, size_t,
                         void *);
+
+typedef int (*q4_product_call)(const slim_group_q4_layer *, const void *, int64_t, int32_t, void *, int64_t, int32_t, void *);
+static q4_product_call call_q4_gemm, call_q4_gemm_t;
+static int (*call_q4_gated)(const slim_group_q4_layer *, const slim_group_q4_layer *, const void *, int64_t, int32_t, void *, int64_t, void *, int64_t, void *,
+                            int64_t, int32_t, void *);
+static int (*call_q4_backward)(const slim_group_q4_layer *, const slim_group_q4_layer *, const void *, int64_t, const void *, int64_t, const void *, int64_t,
+                               int32_t, void *, int64_t, void *, int64_t, void *, int64_t, int32_t, void *);
 
 static int refuse(const char *name, const char *why)
 {
@@ -211,12 +218,134 @@ static PyObject *gemm(PyObject *self, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(status);
 }
 
-/* init((fp16, bf16, fp32, uint8, e4m3), current-stream function, addresses of norm, act, gemm) */
+/* ---- 4-bit layers with a scale for each group of inputs ----
+ * Each call returns a status, or (nothing enqueued) STALE where a layer's tensors are no longer where its struct says, ELSEWHERE where the
+ * tensors' device is not the current one: the caller makes the struct anew, or makes the device current, and calls again.
+ */
+enum { STALE = 1, ELSEWHERE = 2 };
+
+/* A layer is five arguments: its struct's address, its device, its codes, scales and zero points (None: symmetric). */
+static const slim_group_q4_layer *q4_layer(PyObject *const *a, long long *device, int *stale)
+{
+    const slim_group_q4_layer *l = PyLong_AsVoidPtr(a[0]);
+    *device = PyLong_AsLongLong(a[1]);
+    if (PyErr_Occurred()) return NULL;
+    if (!l) return refuse("layer", "has no address"), NULL;
+    const long long cb = ((long long)l->k + 127) / 128, rb = ((long long)l->n + 15) / 16, groups = ((long long)l->k + l->group - 1) / l->group * l->n;
+    if (address(a[2]) != l->codes || number(a[2], s_numel) != rb * cb * 1024 || address(a[3]) != (void *)l->scales || number(a[3], s_numel) != groups)
+        *stale = 1;
+    else if (a[4] == Py_None ? l->zeros != NULL : (address(a[4]) != l->zeros || number(a[4], s_numel) != groups))
+        *stale = 1;
+    return PyErr_Occurred() ? NULL : l;
+}
+
+/* t as [m][k] of a 16-bit type on the device (m, k < 0: any; type < 0: any of the two). */
+static int q4_matrix(PyObject *t, const char *name, long long m, long long k, int type, long long device, matrix *out)
+{
+    if (rows(t, name, out)) return -1;
+    if (out->type != SLIM_F16 && out->type != SLIM_BF16) return refuse(name, "must be float16 or bfloat16");
+    if ((type >= 0 && out->type != type) || out->device != device || (m >= 0 && out->m != m) || (k >= 0 && out->k != k))
+        return refuse(name, "must have the call's type and size, on the layer's device");
+    return 0;
+}
+
+/* 1 where the device is not the current one, -1 with an exception set. */
+static int elsewhere(long long device)
+{
+    PyObject *r = PyObject_CallNoArgs(device_now);
+    if (!r) return -1;
+    const long long now = PyLong_AsLongLong(r);
+    Py_DECREF(r);
+    return PyErr_Occurred() ? -1 : now != device;
+}
+
+/* q4_product(transposed, layer (5), X, Y) */
+static PyObject *q4_product(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    (void)self;
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "q4_product takes 8 arguments");
+    long long device;
+    int stale = 0, status;
+    const int transposed = a[0] == Py_True;
+    const slim_group_q4_layer *l = q4_layer(a + 1, &device, &stale);
+    if (!l) return NULL;
+    if (stale) return PyLong_FromLong(STALE);
+    matrix x, y;
+    void *st;
+    if (q4_matrix(a[6], transposed ? "dY" : "X", -1, transposed ? l->n : l->k, -1, device, &x) ||
+        q4_matrix(a[7], transposed ? "dX" : "Y", x.m, transposed ? l->k : l->n, x.type, device, &y))
+        return NULL;
+    const int away = elsewhere(device);
+    if (away < 0) return NULL;
+    if (away) return PyLong_FromLong(ELSEWHERE);
+    if (stream(device, &st)) return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    status = (transposed ? call_q4_gemm_t : call_q4_gemm)(l, x.p, x.ld, (int32_t)x.m, y.p, y.ld, x.type, st);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* q4_gated(gate (5), up (5), X, H, G, U); G, U may be None */
+static PyObject *q4_gated(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    (void)self;
+    if (n != 14) return PyErr_Format(PyExc_TypeError, "q4_gated takes 14 arguments");
+    long long device, other;
+    int stale = 0, status;
+    const slim_group_q4_layer *gate = q4_layer(a, &device, &stale), *up = gate ? q4_layer(a + 5, &other, &stale) : NULL;
+    if (!up) return NULL;
+    if (stale) return PyLong_FromLong(STALE);
+    if (other != device) return refuse("up", "must be on gate's device"), NULL;
+    matrix x, h, g = {0}, u = {0};
+    void *st;
+    if (q4_matrix(a[10], "X", -1, gate->k, -1, device, &x) || q4_matrix(a[11], "H", x.m, gate->n, x.type, device, &h) ||
+        (a[12] != Py_None && q4_matrix(a[12], "G", x.m, gate->n, x.type, device, &g)) ||
+        (a[13] != Py_None && q4_matrix(a[13], "U", x.m, gate->n, x.type, device, &u)))
+        return NULL;
+    const int away = elsewhere(device);
+    if (away < 0) return NULL;
+    if (away) return PyLong_FromLong(ELSEWHERE);
+    if (stream(device, &st)) return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    status = call_q4_gated(gate, up, x.p, x.ld, (int32_t)x.m, h.p, h.ld, g.p, g.ld, u.p, u.ld, x.type, st);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* q4_backward(gate (5), up (5), dH, G, U, dG, dU, dX) */
+static PyObject *q4_backward(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    (void)self;
+    if (n != 16) return PyErr_Format(PyExc_TypeError, "q4_backward takes 16 arguments");
+    long long device, other;
+    int stale = 0, status;
+    const slim_group_q4_layer *gate = q4_layer(a, &device, &stale), *up = gate ? q4_layer(a + 5, &other, &stale) : NULL;
+    if (!up) return NULL;
+    if (stale) return PyLong_FromLong(STALE);
+    if (other != device) return refuse("up", "must be on gate's device"), NULL;
+    static const char *const names[] = {"dH", "G", "U", "dG", "dU", "dX"};
+    matrix v[6];
+    void *st;
+    for (int i = 0; i < 6; ++i)
+        if (q4_matrix(a[10 + i], names[i], i ? v[0].m : -1, i < 5 ? gate->n : gate->k, i ? v[0].type : -1, device, &v[i])) return NULL;
+    const int away = elsewhere(device);
+    if (away < 0) return NULL;
+    if (away) return PyLong_FromLong(ELSEWHERE);
+    if (stream(device, &st)) return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    status = call_q4_backward(gate, up, v[0].p, v[0].ld, v[1].p, v[1].ld, v[2].p, v[2].ld, (int32_t)v[0].m, v[3].p, v[3].ld, v[4].p, v[4].ld, v[5].p, v[5].ld,
+                              v[0].type, st);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+/* init((fp16, bf16, fp32, uint8, e4m3), current-stream function, current-device function, addresses of norm, act, gemm and of the group operators'
+   gemm, gemm_t, gated, gated_backward) */
 static PyObject *init(PyObject *self, PyObject *args)
 {
     (void)self;
-    PyObject *t[5], *f, *p[3];
-    if (!PyArg_ParseTuple(args, "(OOOOO)OOOO", &t[0], &t[1], &t[2], &t[3], &t[4], &f, &p[0], &p[1], &p[2])) return NULL;
+    PyObject *t[5], *f, *d, *p[7];
+    if (!PyArg_ParseTuple(args, "(OOOOO)OOOOOOOOO", &t[0], &t[1], &t[2], &t[3], &t[4], &f, &d, &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6])) return NULL;
     for (int i = 0; i < 5; ++i) {
         Py_INCREF(t[i]);
         Py_XSETREF(types[i], t[i]);
@@ -226,6 +355,12 @@ static PyObject *init(PyObject *self, PyObject *args)
     *(void **)&call_norm = PyLong_AsVoidPtr(p[0]);
     *(void **)&call_act = PyLong_AsVoidPtr(p[1]);
     *(void **)&call_gemm = PyLong_AsVoidPtr(p[2]);
+    Py_INCREF(d);
+    Py_XSETREF(device_now, d);
+    *(void **)&call_q4_gemm = PyLong_AsVoidPtr(p[3]);
+    *(void **)&call_q4_gemm_t = PyLong_AsVoidPtr(p[4]);
+    *(void **)&call_q4_gated = PyLong_AsVoidPtr(p[5]);
+    *(void **)&call_q4_backward = PyLong_AsVoidPtr(p[6]);
     if (PyErr_Occurred()) return NULL;
     Py_RETURN_NONE;
 }
@@ -234,6 +369,9 @@ static PyMethodDef methods[] = {{"init", init, METH_VARARGS, NULL},
                                 {"norm", (PyCFunction)(void (*)(void))norm, METH_FASTCALL, NULL},
                                 {"act", (PyCFunction)(void (*)(void))act, METH_FASTCALL, NULL},
                                 {"gemm", (PyCFunction)(void (*)(void))gemm, METH_FASTCALL, NULL},
+                                {"q4_product", (PyCFunction)(void (*)(void))q4_product, METH_FASTCALL, NULL},
+                                {"q4_gated", (PyCFunction)(void (*)(void))q4_gated, METH_FASTCALL, NULL},
+                                {"q4_backward", (PyCFunction)(void (*)(void))q4_backward, METH_FASTCALL, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_slim_args", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

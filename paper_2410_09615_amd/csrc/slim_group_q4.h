@@ -1,0 +1,113 @@
+// What the operators on 4-bit weights with a scale for each group of inputs share: the layout of the codes, and codes as numbers.
+#ifndef SLIM_GROUP_Q4_H
+#define SLIM_GROUP_Q4_H
+
+#include "slim_block_fp8.h"
+
+namespace slim {
+
+// Codes are kept in blocks of 16 rows x 128 inputs (1 KiB), row block major.  Piece (q, r) of a block, 16 bytes at (16 q + r) * 16, is what a
+// lane holds of the four 16 x 16 x 32 products over the block's inputs: its dword j has inputs 32 j + 8 q .. + 7 of row r.  Inputs 2 i and
+// 2 i + 1 of a dword are its nibbles i and i + 4, so that shifting by 4 i and masking leaves the two as 16-bit halves.
+constexpr int kGq4Rows = 16, kGq4Cols = 128, kGq4Block = 1024;
+constexpr int kGq4Sym = 8;                    // the zero point of symmetric weights
+
+inline int gq4_row_blocks(int n) { return (int)(((int64_t)n + kGq4Rows - 1) / kGq4Rows); }
+inline int gq4_col_blocks(int k) { return (int)(((int64_t)k + kGq4Cols - 1) / kGq4Cols); }
+inline int gq4_groups(int k, int shift) { return (int)(((int64_t)k + (1 << shift) - 1) >> shift); }
+// 5, 6, 7 for groups of 32, 64, 128; -1 for others
+inline int gq4_shift(int group) { return group == 32 ? 5 : group == 64 ? 6 : group == 128 ? 7 : -1; }
+
+inline bool half_dtype(int32_t d) { return d == SLIM_F16 || d == SLIM_BF16; }
+inline bool whole_elements(const void *p, int32_t d) { return (reinterpret_cast<uintptr_t>(p) & (d == SLIM_F32 ? 3u : 1u)) == 0; }
+
+// One layer's weights as the kernels take them.
+struct Gq4Weights {
+    const uint8_t *codes;
+    const half_t *scales;     // [n][groups]
+    const uint8_t *zeros;     // the same, or null: kGq4Sym throughout
+};
+
+// The layer is what its sizes say it has to be; sets shift.
+inline int gq4_check(const slim_group_q4_layer *l, int *shift)
+{
+    if (!l || !l->codes || !l->scales) return SLIM_ERR_NULL;
+    if (slim_group_q4_sizes(l->n, l->k, l->group, nullptr, nullptr, nullptr) != SLIM_OK) return SLIM_ERR_SHAPE;
+    if (!aligned16(l->codes) || (reinterpret_cast<uintptr_t>(l->scales) & 1u)) return SLIM_ERR_ALIGN;
+    *shift = gq4_shift(l->group);
+    return SLIM_OK;
+}
+inline Gq4Weights gq4_weights(const slim_group_q4_layer *l)
+{
+    return Gq4Weights{l->codes, reinterpret_cast<const half_t *>(l->scales), l->zeros};
+}
+
+// Two codes, in the halves of a dword, as 1024 + code in fp16.
+__device__ __forceinline__ half2_t gq4_biased(uint32_t halves) { return __builtin_bit_cast(half2_t, (halves & 0x000f000fu) | 0x64006400u); }
+
+// What turns codes into values (c - z) s, for the two codes of a pair (of one group or of two).
+//   fp16: c - z exactly, and one rounding of the product to fp16.
+//   bf16: (1024 + c) s - (1024 + z) s by one fused operation in binary32, exact since a code, a zero point and a scale have 23 bits between them; one rounding.
+template <class T>
+struct Gq4Pair;
+template <>
+struct Gq4Pair<F16> {
+    half2_t s, z;
+    __device__ __forceinline__ Gq4Pair() {}
+    __device__ __forceinline__ Gq4Pair(half_t s0, uint32_t z0, half_t s1, uint32_t z1)
+        : s{s0, s1}, z{(half_t)(float)(1024u + z0), (half_t)(float)(1024u + z1)}
+    {
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t halves) const
+    {
+        return __builtin_bit_cast(uint32_t, (gq4_biased(halves) - z) * s);
+    }
+};
+template <>
+struct Gq4Pair<BF16> {
+    float s0, s1, c0, c1;
+    __device__ __forceinline__ Gq4Pair() {}
+    __device__ __forceinline__ Gq4Pair(half_t a, uint32_t z0, half_t b, uint32_t z1) : s0((float)a), s1((float)b)
+    {
+        c0 = -(float)(1024u + z0) * s0;
+        c1 = -(float)(1024u + z1) * s1;
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t halves) const
+    {
+        typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+        const half2_t h = gq4_biased(halves);
+        bf2 v;
+        v[0] = (__bf16)__builtin_fmaf((float)h[0], s0, c0);
+        v[1] = (__bf16)__builtin_fmaf((float)h[1], s1, c1);
+        return __builtin_bit_cast(uint32_t, v);
+    }
+};
+
+template <class T>
+struct Gq4Vec {
+    typedef typename T::type E;
+    typedef E v8 __attribute__((ext_vector_type(8)));
+};
+
+__device__ __forceinline__ float16_t gq4_mma32(Gq4Vec<F16>::v8 a, Gq4Vec<F16>::v8 b, float16_t c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float16_t gq4_mma32(Gq4Vec<BF16>::v8 a, Gq4Vec<BF16>::v8 b, float16_t c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float4_t gq4_mma16(Gq4Vec<F16>::v8 a, Gq4Vec<F16>::v8 b, float4_t c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float4_t gq4_mma16(Gq4Vec<BF16>::v8 a, Gq4Vec<BF16>::v8 b, float4_t c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// silu(g) = g sigma(g)
+__device__ __forceinline__ float gq4_sigma(float g) { return 1.f / (1.f + __expf(-g)); }
+
+}  // namespace slim
+#endif
