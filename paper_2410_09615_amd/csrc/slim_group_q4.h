@@ -10,6 +10,7 @@ namespace slim {
 // lane holds of the four 16 x 16 x 32 products over the block's inputs: its dword j has inputs 32 j + 8 q .. + 7 of row r.  Inputs 2 i and
 // 2 i + 1 of a dword are its nibbles i and i + 4, so that shifting by 4 i and masking leaves the two as 16-bit halves.
 constexpr int kGq4Rows = 16, kGq4Cols = 128, kGq4Block = 1024;
+constexpr int kGq4Few = 48;                   // tokens up to which weights are streamed
 constexpr int kGq4Sym = 8;                    // the zero point of symmetric weights
 
 inline int gq4_row_blocks(int n) { return (int)(((int64_t)n + kGq4Rows - 1) / kGq4Rows); }

@@ -260,6 +260,11 @@ static int launch_gq4(const Gq4TileArgs &a, int shift, int32_t dtype, hipStream_
 int gq4_launch_act_backward(const void *dH, int64_t h_ld, const void *G, int64_t g_ld, const void *U, int64_t u_ld, int32_t m, int32_t n, void *dG,
                             int64_t dg_ld, void *dU, int64_t du_ld, int32_t dtype, hipStream_t st);
 
+// Weights are streamed for up to so many tokens (whose row stride leaves a token within 32 bits of the first).
+static bool gq4_few(int m, int64_t x_ld) { return m <= kGq4Few && x_ld < (1 << 24); }
+int gq4_launch_stream(const slim_group_q4_layer *layer, const slim_group_q4_layer *up, int shift, const void *X, int64_t x_ld, int32_t m, void *const (&y)[3],
+                      const int64_t (&y_ld)[3], int32_t dtype, hipStream_t st);
+
 static Gq4TileArgs gq4_args(const slim_group_q4_layer *l, int shift, int m)
 {
     Gq4TileArgs a{};
@@ -301,6 +306,7 @@ extern "C" int slim_group_q4_gemm(const slim_group_q4_layer *layer, const void *
     a.x_ld[0] = x_ld;
     a.y[0] = Y;
     a.y_ld[0] = y_ld;
+    if (gq4_few(m, x_ld)) return gq4_launch_stream(layer, nullptr, shift, X, x_ld, m, a.y, a.y_ld, dtype, static_cast<hipStream_t>(stream));
     return launch_gq4<kGq4Plain>(a, shift, dtype, static_cast<hipStream_t>(stream));
 }
 
@@ -340,6 +346,7 @@ extern "C" int slim_group_q4_gated(const slim_group_q4_layer *gate, const slim_g
     a.y_ld[1] = g_ld;
     a.y[2] = U;
     a.y_ld[2] = u_ld;
+    if (gq4_few(m, x_ld)) return gq4_launch_stream(gate, up, shift, X, x_ld, m, a.y, a.y_ld, dtype, static_cast<hipStream_t>(stream));
     return launch_gq4<kGq4Gated>(a, shift, dtype, static_cast<hipStream_t>(stream));
 }
 
