@@ -43,45 +43,82 @@ inline Gq4Weights gq4_weights(const slim_group_q4_layer *l)
     return Gq4Weights{l->codes, reinterpret_cast<const half_t *>(l->scales), l->zeros};
 }
 
-// Two codes, in the halves of a dword, as 1024 + code in fp16.
-__device__ __forceinline__ half2_t gq4_biased(uint32_t halves) { return __builtin_bit_cast(half2_t, (halves & 0x000f000fu) | 0x64006400u); }
+// Constants that the compiler has to keep in registers: an instruction takes no two of them as literals.
+struct Gq4Masks {
+    uint32_t low, high, bias;
+    half2_t sixteenth;
+    __device__ __forceinline__ Gq4Masks()
+    {
+        low = 0x000f000fu;
+        high = 0x00f000f0u;
+        bias = 0x64006400u;
+        sixteenth = half2_t{(half_t)0.0625f, (half_t)0.0625f};
+        asm volatile("" : "+s"(low), "+s"(high), "+v"(bias), "+v"(sixteenth));
+    }
+};
 
-// What turns codes into values (c - z) s, for the two codes of a pair (of one group or of two).
+// Nibble E (0 .. 3) of both halves of a dword in fp16: 1024 + c of an even one, 1024 + 16 c of an odd one (the bits of 1024 set beside it): a shift per two nibbles.
+template <int E>
+__device__ __forceinline__ half2_t gq4_biased(uint32_t d, const Gq4Masks &k)
+{
+    return __builtin_bit_cast(half2_t, ((E < 2 ? d : d >> 8) & (E % 2 ? k.high : k.low)) | k.bias);
+}
+// 1024 + z of two zero points in fp16 (up to 1024 the steps there are 1)
+__device__ __forceinline__ half2_t gq4_biased_zeros(uint32_t z0, uint32_t z1) { return __builtin_bit_cast(half2_t, (z1 << 16 | z0) + 0x64006400u); }
+
+// c - z of nibble E of both halves, exactly; z: 1024 + the zero points.
+template <int E>
+__device__ __forceinline__ half2_t gq4_less_zeros(uint32_t d, const Gq4Masks &k, half2_t z, half2_t z_sixteenth)
+{
+    const half2_t c = gq4_biased<E>(d, k);
+    return E % 2 ? __builtin_elementwise_fma(c, k.sixteenth, -z_sixteenth) : c - z;
+}
+
+// What turns codes into values (c - z) s, for the two halves (of one group or of two).
 //   fp16: c - z exactly, and one rounding of the product to fp16.
 //   bf16: (1024 + c) s - (1024 + z) s by one fused operation in binary32, exact since a code, a zero point and a scale have 23 bits between them; one rounding.
 template <class T>
 struct Gq4Pair;
 template <>
 struct Gq4Pair<F16> {
-    half2_t s, z;
-    __device__ __forceinline__ Gq4Pair() {}
+    half2_t s, z, z16;
     __device__ __forceinline__ Gq4Pair(half_t s0, uint32_t z0, half_t s1, uint32_t z1)
-        : s{s0, s1}, z{(half_t)(float)(1024u + z0), (half_t)(float)(1024u + z1)}
+        : s{s0, s1}, z(gq4_biased_zeros(z0, z1)), z16(z - half2_t{(half_t)960.f, (half_t)960.f})
     {
     }
-    __device__ __forceinline__ uint32_t operator()(uint32_t halves) const
+    template <int E>
+    __device__ __forceinline__ uint32_t value(uint32_t d, const Gq4Masks &k) const
     {
-        return __builtin_bit_cast(uint32_t, (gq4_biased(halves) - z) * s);
+        return __builtin_bit_cast(uint32_t, gq4_less_zeros<E>(d, k, z, z16) * s);
     }
 };
 template <>
 struct Gq4Pair<BF16> {
-    float s0, s1, c0, c1;
-    __device__ __forceinline__ Gq4Pair() {}
+    float s0, s1, c0, c1, o0, o1;                 // scales; what an even nibble's value lacks, and an odd one's
     __device__ __forceinline__ Gq4Pair(half_t a, uint32_t z0, half_t b, uint32_t z1) : s0((float)a), s1((float)b)
     {
         c0 = -(float)(1024u + z0) * s0;
         c1 = -(float)(1024u + z1) * s1;
+        o0 = -(float)(64u + z0) * s0;
+        o1 = -(float)(64u + z1) * s1;
     }
-    __device__ __forceinline__ uint32_t operator()(uint32_t halves) const
+    template <int E>
+    __device__ __forceinline__ uint32_t value(uint32_t d, const Gq4Masks &k) const
     {
         typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
-        const half2_t h = gq4_biased(halves);
+        const half2_t h = gq4_biased<E>(d, k);
+        const float f = E % 2 ? 0.0625f : 1.f;
         bf2 v;
-        v[0] = (__bf16)__builtin_fmaf((float)h[0], s0, c0);
-        v[1] = (__bf16)__builtin_fmaf((float)h[1], s1, c1);
+        v[0] = (__bf16)__builtin_fmaf((float)h[0], s0 * f, E % 2 ? o0 : c0);
+        v[1] = (__bf16)__builtin_fmaf((float)h[1], s1 * f, E % 2 ? o1 : c1);
         return __builtin_bit_cast(uint32_t, v);
     }
+};
+
+// A value at any address.
+template <class V>
+struct __attribute__((packed, aligned(1))) Gq4Any {
+    V v;
 };
 
 template <class T>

@@ -20,46 +20,20 @@ struct Gq4StreamArgs {
     int n, k, m, cb, rb, kg;
 };
 
-// Constants that the compiler has to keep in registers: an instruction takes no two of them as literals.
-struct Gq4Masks {
-    uint32_t low, high, bias;
-    half2_t sixteenth;
-    __device__ __forceinline__ Gq4Masks()
-    {
-        low = 0x000f000fu;
-        high = 0x00f000f0u;
-        bias = 0x64006400u;
-        sixteenth = half2_t{(half_t)0.0625f, (half_t)0.0625f};
-        asm volatile("" : "+s"(low), "+s"(high), "+v"(bias), "+v"(sixteenth));
-    }
-};
-
-// c - z of the eight codes of a dword, exactly, in the inputs' type; z0: 1024 + z twice, z1: 64 + z twice.  A code in the low four bits of a half is 1024 + c once the
-// bits of 1024 are set beside it, one in the next four 1024 + 16 c, which a sixteenth makes 64 + c: one shift per four pairs.
+// c - z of the eight codes of a dword, exactly, in the inputs' type.
 template <class T>
 __device__ __forceinline__ typename Gq4Vec<T>::v8 gq4_whole(uint32_t d, const Gq4Masks &k, half2_t z0, half2_t z1)
 {
     uint4_t v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const uint32_t h = e < 2 ? d : d >> 8;
-        half2_t c;
-        if (e % 2 == 0)
-            c = __builtin_bit_cast(half2_t, (h & k.low) | k.bias) - z0;
-        else
-            c = __builtin_elementwise_fma(__builtin_bit_cast(half2_t, (h & k.high) | k.bias), k.sixteenth, -z1);
-        if constexpr (sizeof(typename T::type) == 2 && !__is_same(T, BF16))
-            v[e] = __builtin_bit_cast(uint32_t, c);
-        else
-            v[e] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, (float)c[1]), __builtin_bit_cast(uint32_t, (float)c[0]), 0x07060302u);
-    }
+    static_for<4>([&](auto ec) {
+        const half2_t c = gq4_less_zeros<decltype(ec)::value>(d, k, z0, z1);
+        if constexpr (__is_same(T, F16))
+            v[decltype(ec)::value] = __builtin_bit_cast(uint32_t, c);
+        else                                                          // (whole numbers below 256: their first 16 bits in binary32)
+            v[decltype(ec)::value] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, (float)c[1]), __builtin_bit_cast(uint32_t, (float)c[0]), 0x07060302u);
+    });
     return __builtin_bit_cast(typename Gq4Vec<T>::v8, v);
 }
-
-template <class V>
-struct __attribute__((packed, aligned(1))) Gq4Any {
-    V v;
-};
 
 // Orders a wavefront's writes to LDS before its reads of what other lanes wrote: its LDS instructions are executed in order.
 __device__ __forceinline__ void wave_lds_order()
@@ -181,7 +155,7 @@ __global__ __launch_bounds__(THREADS) void gq4_stream_kernel(Gq4StreamArgs a)
                 const uint8_t *table = own + Lds::scales + f * Lds::table;
                 s[f] = (float)*reinterpret_cast<const half_t *>(table + r * Lds::scale_row + (at + g) * 2);
                 const uint32_t zp = table[16 * Lds::scale_row + r * Lds::zero_row + at + g];
-                z0[f] = __builtin_bit_cast(half2_t, zp * 0x10001u + 0x64006400u);
+                z0[f] = gq4_biased_zeros(zp, zp);
                 z1[f] = z0[f] - half2_t{(half_t)960.f, (half_t)960.f};
 #pragma unroll
                 for (int t = 0; t < TB; ++t) p[f][t] = float4_t{0.f, 0.f, 0.f, 0.f};

@@ -29,11 +29,25 @@ struct Gq4TileArgs {
 // order is the same 32 rows on.
 __device__ __forceinline__ uint32_t gq4_turn(uint32_t row) { return (row & 7u) ^ (row >> 3 & 3u); }
 
+// Per group of wavefronts: two buffers of a piece's weights and tokens, two windows of scales and zero points.
+template <int MODE, int KG, int BO, int BT>
+struct Gq4TileLds {
+    static constexpr int table = MODE == kGq4Transposed ? 8 * 64 * 3 : BO * 24, bytes = KG * (2 * (BO + BT) * 128 + 2 * table);
+};
+
+// A barrier for what is in LDS: unlike __syncthreads() it does not wait for loads that are under way to registers.
+__device__ __forceinline__ void gq4_lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+}
+
 // How the loop over the inputs is laid out.  KG groups of WR x WT wavefronts take turns at pieces of 64 inputs, each with two buffers of its own in LDS.  While a
 // piece is multiplied from one buffer, the next one goes from registers into the other, codes becoming numbers on the way, and the one after that is asked for from
 // memory into the registers that this frees: every quarter of a piece's products (16 inputs) has a quarter of that work beside it.  One barrier per piece.
 // Inputs that end inside a piece are left for last and taken without that overlap.
-template <class T, int MODE, int SHIFT, int KG, int WR, int WT, int AF, int BF>
+template <class T, int MODE, int SHIFT, int KG, int P, int WR, int WT, int AF, int BF>
 __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_tile_kernel(Gq4TileArgs a)
 {
     typedef typename T::type E;
@@ -52,72 +66,106 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_tile_kernel(Gq4TileA
     const int o0 = tile % a.tiles_o * (GATED ? BO / 2 : BO), t0 = tile / a.tiles_o * BT;
     const int len = TRANS ? a.n : a.k, outs = TRANS ? a.k : a.n;                 // what is summed over; results of a token
     const int whole = len / 64, terms = TRANS ? a.terms : 1, steps = whole * terms;
-    uint8_t *const own = lds + group * (2 * STAGE);
+    const Gq4Masks masks;
+    constexpr int TABLE = Gq4TileLds<MODE, KG, BO, BT>::table;
+    uint8_t *const own = lds + group * (2 * STAGE + 2 * TABLE), *const tables = own + 2 * STAGE;
 
     // ---- where this thread's share of a piece lies: uniform bases, and 32 bits from there on ----
-    uint32_t x_at[XTASKS], w_at[WTASKS], s_at[WTASKS];
+    uint32_t x_at[XTASKS];
     const uint8_t *codes[WTASKS];
-    const half_t *scales[WTASKS];
-    const uint8_t *zeros[WTASKS];
 #pragma unroll
-    for (int i = 0; i < XTASKS; ++i) {
-        const int task = tid + i * THREADS;
-        x_at[i] = (uint32_t)min(task >> 3, a.m - 1 - t0);                        // (times the row's length, which a term has its own of)
-    }
+    for (int i = 0; i < XTASKS; ++i) x_at[i] = (uint32_t)min((tid + i * THREADS) >> 3, a.m - 1 - t0);      // (times the row's length, which a term has its own of)
+    const uint32_t w_at = TRANS ? (uint32_t)(((lane >> 4) * 16 + 4 * (lane >> 2 & 3)) * 16 + (lane & 3) * 4) : (uint32_t)lane * 16u;
     auto weights = [&](int term) {
 #pragma unroll
         for (int i = 0; i < WTASKS; ++i) {
             const int b = gw + i * (WR * WT);                                     // the block of 16 x 128 this wavefront has a part of
             if constexpr (!TRANS) {
-                const int r = lane & 15, rb = min(GATED ? o0 / 16 + (b >> 2) * 2 + (b & 1) : o0 / 16 + b, a.rb - 1);
-                const Gq4Weights &w = GATED && (b & 2) ? a.w[1] : a.w[0];
-                codes[i] = w.codes + (int64_t)rb * a.cb * kGq4Block;
-                w_at[i] = (uint32_t)lane * 16u;
-                scales[i] = w.scales + (int64_t)rb * kGq4Rows * a.kg;
-                zeros[i] = w.zeros ? w.zeros + (int64_t)rb * kGq4Rows * a.kg : nullptr;
-                s_at[i] = (uint32_t)min(r, a.n - 1 - rb * kGq4Rows) * (uint32_t)a.kg;
+                const int rb = min(GATED ? o0 / 16 + (b >> 2) * 2 + (b & 1) : o0 / 16 + b, a.rb - 1);
+                codes[i] = (GATED && (b & 2) ? a.w[1].codes : a.w[0].codes) + (int64_t)rb * a.cb * kGq4Block;
             } else {
-                const int j = lane & 3, p = lane >> 2 & 3, q = lane >> 4, rl = b & 3, cb = min(o0 / 128 + (b >> 2), a.cb - 1);
-                const Gq4Weights &w = a.w[term];
-                codes[i] = w.codes + ((int64_t)rl * a.cb + cb) * kGq4Block;
-                w_at[i] = (uint32_t)((q * 16 + 4 * p) * 16 + j * 4);
-                scales[i] = w.scales + (int64_t)rl * kGq4Rows * a.kg;
-                zeros[i] = w.zeros ? w.zeros + (int64_t)rl * kGq4Rows * a.kg : nullptr;
-                s_at[i] = (uint32_t)(4 * p) * (uint32_t)a.kg + (uint32_t)min((cb * 128 + 32 * j) >> SHIFT, a.kg - 1);
+                const int cb = min(o0 / 128 + (b >> 2), a.cb - 1);
+                codes[i] = (term ? a.w[1].codes : a.w[0].codes) + ((int64_t)(b & 3) * a.cb + cb) * kGq4Block;
             }
         }
     };
 
-    vec8 xv[XTASKS];
-    uint32_t wv[WTASKS][PARTS], zv[WTASKS][PARTS];
-    half_t sv[WTASKS][PARTS];
+    struct Piece64 {                                                             // a thread's share of a piece, in registers
+        vec8 x[XTASKS];
+        uint32_t w[WTASKS][PARTS];
+    };
+    Piece64 pieces[P];
     // of the term's inputs from `at` on: task i of the tokens, task i of the weights
-    auto fetch_x = [&](int i, int term, int at) {
+    auto fetch_x = [&](Piece64 &v, int i, int term, int at) {
         const uint8_t *base = static_cast<const uint8_t *>(term ? a.x[1] : a.x[0]);
         const int64_t ld = term ? a.x_ld[1] : a.x_ld[0];
         base += ((int64_t)t0 * ld + at) * 2;
-        xv[i] = Piece<T, 8>::load(reinterpret_cast<const E *>(base + (x_at[i] * (uint32_t)ld + (uint32_t)(tid & 7) * 8u) * 2u));
+        v.x[i] = Piece<T, 8>::load(reinterpret_cast<const E *>(base + (x_at[i] * (uint32_t)ld + (uint32_t)(tid & 7) * 8u) * 2u));
     };
-    auto fetch_w = [&](int i, int at) {
+    auto fetch_w = [&](Piece64 &v, int i, int at) {
         if constexpr (!TRANS) {
-            const uint2_t d = *reinterpret_cast<const uint2_t *>(codes[i] + ((int64_t)(at >> 7) * kGq4Block + (at & 64) / 8) + w_at[i]);
-            wv[i][0] = d[0];
-            wv[i][1] = d[1];
-#pragma unroll
-            for (int j = 0; j < (SHIFT == 5 ? 2 : 1); ++j) {
-                const int gi = (at + 32 * j) >> SHIFT;
-                sv[i][j] = *(scales[i] + gi + s_at[i]);
-                zv[i][j] = zeros[i] ? (uint32_t) * (zeros[i] + gi + s_at[i]) : (uint32_t)kGq4Sym;
-            }
+            const uint2_t d = *reinterpret_cast<const uint2_t *>(codes[i] + ((int64_t)(at >> 7) * kGq4Block + (at & 64) / 8) + w_at);
+            v.w[i][0] = d[0];
+            v.w[i][1] = d[1];
         } else {
             const uint8_t *c = codes[i] + (int64_t)(at >> 4) * a.cb * kGq4Block;
-            const half_t *s = scales[i] + (int64_t)at * a.kg;
-            const uint8_t *z = zeros[i] + (int64_t)at * a.kg;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                wv[i][e] = *reinterpret_cast<const uint32_t *>(c + 16 * e + w_at[i]);
-                sv[i][e] = *(s + (int64_t)e * a.kg + s_at[i]);
-                zv[i][e] = zeros[i] ? (uint32_t) * (z + (int64_t)e * a.kg + s_at[i]) : (uint32_t)kGq4Sym;
+            for (int e = 0; e < 4; ++e) v.w[i][e] = *reinterpret_cast<const uint32_t *>(c + 16 * e + w_at);
+        }
+    };
+    // ---- scales and zero points: windows of them in LDS, two, filled one ahead ----
+    // Where each lane fetches the scale of its own row, neighbouring lanes ask the memory pipeline for different lines, which takes four times as long as when they share
+    // one: so eight groups of a row are fetched by eight lanes (forward; a window is 8 groups of the tile's rows), or those of the tile's columns (transposed; a window is
+    // the 64 rows of a piece).  Forward the table is [row][8 groups], transposed [group][64 rows].
+    constexpr int SPAN = TRANS ? (BO >> SHIFT) : 8, ITEMS = ((TRANS ? 64 : BO) * SPAN + THREADS - 1) / THREADS;
+    static_assert(SPAN <= 8, "window");
+    struct Window {
+        half_t s[ITEMS];
+        uint32_t z[ITEMS];
+        int term;
+    };
+    Window ahead;
+    // forward: window w; transposed: rows from `at` on of the term's layer
+    auto load_window = [&](int w, int term, int at) {
+        ahead.term = term;
+        const int wave_row = gw * kWave / SPAN;                                  // (a wavefront's items of one i are of one layer)
+        int own_tid = tid;                                                       // (made anew here each time: kept over the loop, what follows from it takes too many registers)
+        asm volatile("" : "+v"(own_tid));
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int item = own_tid + i * THREADS, row = item / SPAN, g = item % SPAN;
+            const Gq4Weights &l = TRANS ? (term ? a.w[1] : a.w[0]) : (GATED && (i * THREADS / SPAN + wave_row & 32) ? a.w[1] : a.w[0]);
+            int local = row, from = 8 * w + g, first = o0;                       // rows from the first one there
+            if constexpr (TRANS) {
+                first = at;
+                from = (o0 >> SHIFT) + g;
+            } else if constexpr (GATED)
+                local = (row >> 6) * 32 + (row & 31);
+            const uint8_t *scales = reinterpret_cast<const uint8_t *>(l.scales + (int64_t)first * a.kg);
+            const uint8_t *zeros = l.zeros ? l.zeros + (int64_t)first * a.kg : scales;      // (symmetric: what is read of the scales instead is not used)
+            const uint32_t place = (uint32_t)min(local, a.n - 1 - first) * (uint32_t)a.kg + (uint32_t)min(from, a.kg - 1);
+            ahead.s[i] = *reinterpret_cast<const half_t *>(scales + place * 2u);
+            ahead.z[i] = *(zeros + place);
+            if constexpr (BO * BT >= 256 * 256) __builtin_amdgcn_sched_barrier(0);          // (one after the other: no registers are left)
+        }
+    };
+    // the first `there` rows of a transposed window are there: the others are no terms of the sum
+    auto put_window = [&](int w, int there) {
+        uint8_t *const t = tables + (w & 1) * TABLE;
+        int own_tid = tid;
+        asm volatile("" : "+v"(own_tid));
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int item = own_tid + i * THREADS, row = item / SPAN, g = item % SPAN;
+            if (TRANS && item >= 64 * SPAN) continue;
+            const bool points = TRANS ? (ahead.term ? a.w[1].zeros : a.w[0].zeros) != nullptr : (GATED && (row & 32) ? a.w[1].zeros : a.w[0].zeros) != nullptr;
+            const uint8_t z = points ? (uint8_t)ahead.z[i] : (uint8_t)kGq4Sym;
+            if constexpr (TRANS) {
+                *reinterpret_cast<half_t *>(t + (g * 64 + row) * 2) = row < there ? ahead.s[i] : (half_t)0.f;
+                t[8 * 64 * 2 + g * 64 + row] = z;
+            } else {
+                *reinterpret_cast<half_t *>(t + row * 24 + g * 2) = ahead.s[i];
+                t[row * 24 + 16 + g] = z;
             }
         }
     };
@@ -128,30 +176,39 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_tile_kernel(Gq4TileA
         const uint32_t row = (uint32_t)(tid + i * THREADS) >> 3;
         xl_at[i] = BO * 128u + row * 128u + (((uint32_t)tid & 7u) ^ gq4_turn(row)) * 16u;
     }
-    auto put_x = [&](int i, uint8_t *to) { *reinterpret_cast<vec8 *>(to + xl_at[i]) = xv[i]; };
-    // quarter `h` of a weight task: forward a half of dword h / 2's work is not worth splitting: dword h / 2 at even h; transposed inputs 2 h and 2 h + 1 of the four rows
-    auto put_w = [&](int i, int h, uint8_t *to) {
+    // (a group with a step less than others multiplies by zeros in the last turn: with a branch around its loads the compiler would wait for all of them each time)
+    auto put_x = [&](const Piece64 &v, int i, uint8_t *to, bool there) {
+        *reinterpret_cast<uint4_t *>(to + xl_at[i]) = there ? __builtin_bit_cast(uint4_t, v.x[i]) : uint4_t{0, 0, 0, 0};
+    };
+    // A quarter of a weight task: forward, dword h / 2 (at even h); transposed, inputs 2 h and 2 h + 1 of the four rows.  Inputs from `at` on, window w.
+    auto put_w = [&](const Piece64 &v, int i, int h, uint8_t *to, int at, int w) {
         const uint32_t b = (uint32_t)(gw + i * (WR * WT));
+        const uint8_t *const t = tables + (w & 1) * TABLE;
         if constexpr (!TRANS) {
             if (h & 1) return;
-            const int j = h / 2, js = SHIFT == 5 ? j : 0;
-            const uint32_t q = (uint32_t)lane >> 4, row = b * 16 + (lane & 15);
-            const Gq4Pair<T> value(sv[i][js], zv[i][js], sv[i][js], zv[i][js]);
-            uint4_t v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = value(wv[i][j] >> (4 * e));
-            *reinterpret_cast<uint4_t *>(to + row * 128 + ((4u * j + q) ^ gq4_turn(row)) * 16) = v;
+            const int j = h / 2;
+            const uint32_t q = (uint32_t)lane >> 4, row = b * 16 + (lane & 15), g = (uint32_t)(at + 32 * j) >> SHIFT & 7u;
+            const half_t sc = *reinterpret_cast<const half_t *>(t + row * 24 + g * 2);
+            const uint32_t z = t[row * 24 + 16 + g];
+            const Gq4Pair<T> value(sc, z, sc, z);
+            uint4_t out;
+            static_for<4>([&](auto e) { out[decltype(e)::value] = value.template value<decltype(e)::value>(v.w[i][j], masks); });
+            *reinterpret_cast<uint4_t *>(to + row * 128 + ((4u * j + q) ^ gq4_turn(row)) * 16) = out;
         } else {
-            const uint32_t j = lane & 3, p = lane >> 2 & 3, q = lane >> 4, piece = (b & 3) * 2 + (p >> 1);
-            const Gq4Pair<T> v01(sv[i][0], zv[i][0], sv[i][1], zv[i][1]), v23(sv[i][2], zv[i][2], sv[i][3], zv[i][3]);
-#pragma unroll
-            for (int e = 2 * h; e < 2 * h + 2; ++e) {
+            const uint32_t j = lane & 3, p = lane >> 2 & 3, q = lane >> 4, piece = (b & 3) * 2 + (p >> 1), g = ((b >> 2) * 128 + 32 * j) >> SHIFT;
+            typedef half_t half4v __attribute__((ext_vector_type(4)));
+            const half4v sc = *reinterpret_cast<const half4v *>(t + (g * 64 + (b & 3) * 16 + 4 * p) * 2);
+            const uint32_t z = *reinterpret_cast<const uint32_t *>(t + 8 * 64 * 2 + g * 64 + (b & 3) * 16 + 4 * p);
+            const Gq4Pair<T> v01(sc[0], z & 255u, sc[1], z >> 8 & 255u), v23(sc[2], z >> 16 & 255u, sc[3], z >> 24);
+            static_for<8>([&](auto ec) {
+                constexpr int e = decltype(ec)::value;
+                if (e / 2 != h) return;
                 const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;          // the nibbles of input e of both rows, as halves
-                const uint32_t d01 = __builtin_amdgcn_perm(wv[i][1], wv[i][0], sel), d23 = __builtin_amdgcn_perm(wv[i][3], wv[i][2], sel);
+                const uint32_t d01 = __builtin_amdgcn_perm(v.w[i][1], v.w[i][0], sel), d23 = __builtin_amdgcn_perm(v.w[i][3], v.w[i][2], sel);
                 const uint32_t col = (b >> 2) * 128 + 32 * j + 8 * q + e;
-                const uint2_t v = {v01(d01 >> (4 * (e >> 1))), v23(d23 >> (4 * (e >> 1)))};
-                *reinterpret_cast<uint2_t *>(to + col * 128 + (piece ^ gq4_turn(col)) * 16 + (p & 1) * 8) = v;
-            }
+                const uint2_t out = {v01.template value<e / 2>(d01, masks), v23.template value<e / 2>(d23, masks)};
+                *reinterpret_cast<uint2_t *>(to + col * 128 + (piece ^ gq4_turn(col)) * 16 + (p & 1) * 8) = out;
+            });
         }
     };
 
@@ -193,94 +250,125 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_tile_kernel(Gq4TileA
             loaded = term;
         }
     };
+    // The window of step s, whose inputs are from `at` on: of the eight groups there, or of the step's rows.
+    auto window_of = [&](int s, int at) { return TRANS ? s : at >> (SHIFT + 3); };
+    auto load_window_of = [&](int w) {
+        int term = 0, at = 0;
+        if constexpr (TRANS) place(w, term, at);
+        load_window(w, term, at);
+    };
     if (steps > 0) {
-        int term, at;
+        int term, at, put_at;
+        load_window_of(0);
         place(0, term, at);
         use_term(term);
 #pragma unroll
-        for (int i = 0; i < XTASKS; ++i) fetch_x(i, term, at);
+        for (int i = 0; i < XTASKS; ++i) fetch_x(pieces[0], i, term, at);
 #pragma unroll
-        for (int i = 0; i < WTASKS; ++i) fetch_w(i, at);
+        for (int i = 0; i < WTASKS; ++i) fetch_w(pieces[0], i, at);
+        put_window(0, 64);
+        load_window_of(1);
+        put_window(1, 64);
+        load_window_of(2);
+        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < XTASKS; ++i) put_x(i, own);
+        for (int i = 0; i < XTASKS; ++i) put_x(pieces[0], i, own, KG == 1 || mine > 0);
 #pragma unroll
         for (int i = 0; i < WTASKS; ++i)
 #pragma unroll
-            for (int h = 0; h < 4; ++h) put_w(i, h, own);
-        place(1, term, at);
-        use_term(term);
+            for (int h = 0; h < 4; ++h) put_w(pieces[0], i, h, own, at, 0);
 #pragma unroll
-        for (int i = 0; i < XTASKS; ++i) fetch_x(i, term, at);
-#pragma unroll
-        for (int i = 0; i < WTASKS; ++i) fetch_w(i, at);
-        __syncthreads();
-        for (int s = 0; s < turns; ++s) {
-            uint8_t *const from = own + (s & 1) * STAGE, *const to = own + (~s & 1) * STAGE;
-            place(s + 2, term, at);
+        for (int n = 1; n <= P; ++n) {
+            place(n, term, at);
             use_term(term);
-            if (s < mine) {
-                vec8 af[2][AF], bf[2][BF];
-                read(from, 0, af[0], bf[0]);
+#pragma unroll
+            for (int i = 0; i < XTASKS; ++i) fetch_x(pieces[n % P], i, term, at);
+#pragma unroll
+            for (int i = 0; i < WTASKS; ++i) fetch_w(pieces[n % P], i, at);
+        }
+        int window = 0;
+        gq4_lds_barrier();
+        vec8 af[2][AF], bf[2][BF];
+        read(own, 0, af[0], bf[0]);
+        for (int s = 0; s < turns;) {
+#pragma unroll
+            for (int n = 1; n <= P; ++n) {
+                uint8_t *const from = own + (s & 1) * STAGE, *const to = own + (~s & 1) * STAGE;
+                Piece64 &next = pieces[n % P];
+                place(s + 1, term, put_at);
+                if (window_of(s + 1, put_at) != window) {
+                    window = window_of(s + 1, put_at);
+                    put_window(window + 1, 64);
+                    load_window_of(window + 2);
+                }
+                place(s + 1 + P, term, at);
+                use_term(term);
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk) {
-                    if (kk < 3) read(from, kk + 1, af[(kk + 1) & 1], bf[(kk + 1) & 1]);
+                    // The barrier stands before the last quarter's products: past it the next piece is in LDS, and its first operands are read beside them.
+                    if (kk == 3) gq4_lds_barrier();
+                    read(kk < 3 ? from : to, (kk + 1) & 3, af[(kk + 1) & 1], bf[(kk + 1) & 1]);
 #pragma unroll
                     for (int i = 0; i < XTASKS; ++i)
-                        if (i * 4 / XTASKS == kk) {
-                            put_x(i, to);
-                            fetch_x(i, term, at);
+                        if (i * 3 / XTASKS == kk) {
+                            put_x(next, i, to, KG == 1 || s + 1 < mine);
+                            fetch_x(next, i, term, at);
                         }
 #pragma unroll
                     for (int i = 0; i < WTASKS; ++i) {
-                        put_w(i, kk, to);
-                        if (kk == 3) fetch_w(i, at);
+#pragma unroll
+                        for (int h = 0; h < 4; ++h)
+                            if ((i * 4 + h) * 3 / (WTASKS * 4) == kk) put_w(next, i, h, to, put_at, window);
+                        if (kk == 3) fetch_w(next, i, at);
                     }
                     multiply(af[kk & 1], bf[kk & 1]);
+                    if constexpr (AF * BF >= 8) {
+#pragma unroll
+                        for (int i = 0; i < AF * BF; ++i) {
+                            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);       // a product
+                            __builtin_amdgcn_sched_group_barrier(0x080, 2, 0);       // LDS
+                            __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);       // vector instructions
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
+                if (++s >= turns) break;
             }
-            __syncthreads();
         }
     }
     if (len % 64) {
-        const int at = whole * 64;
+        const int at = whole * 64, w = window_of(0, at);
         for (int term = 0; term < terms; ++term) {
+            if (TRANS && term != loaded) {
+                weights(term);
+                loaded = term;
+            }
+            load_window(w, term, at);
+            __syncthreads();                                                     // (nobody reads from LDS any more)
+            put_window(w, len - at);
             __syncthreads();
             if (group == 0) {
-                use_term(term);
                 const E *x = static_cast<const E *>(term ? a.x[1] : a.x[0]);
                 const int64_t ld = term ? a.x_ld[1] : a.x_ld[0];
+                Piece64 &v = pieces[0];
 #pragma unroll
                 for (int i = 0; i < XTASKS; ++i) {
                     const E *row = x + ((int64_t)t0 + x_at[i]) * ld;
                     const int c = at + (tid & 7) * 8;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) xv[i][e] = c + e < len ? row[c + e] : (E)0.f;
-                    put_x(i, own);
+                    for (int e = 0; e < 8; ++e) v.x[i][e] = c + e < len ? row[c + e] : (E)0.f;
+                    put_x(v, i, own, true);
                 }
 #pragma unroll
                 for (int i = 0; i < WTASKS; ++i) {
-                    if constexpr (!TRANS) {
-                        const uint2_t d = *reinterpret_cast<const uint2_t *>(codes[i] + ((int64_t)(at >> 7) * kGq4Block + (at & 64) / 8) + w_at[i]);
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const int gi = min((at + 32 * j) >> SHIFT, a.kg - 1);
-                            wv[i][j] = d[j];
-                            sv[i][j] = *(scales[i] + gi + s_at[i]);
-                            zv[i][j] = zeros[i] ? (uint32_t) * (zeros[i] + gi + s_at[i]) : (uint32_t)kGq4Sym;
-                        }
-                    } else {
-                        const int rl = (gw + i * (WR * WT)) & 3, p = lane >> 2 & 3, block = min((at >> 4) + rl, a.rb - 1) - rl;
-                        const uint8_t *c = codes[i] + (int64_t)block * a.cb * kGq4Block;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int row = at + rl * 16 + 4 * p + e, up = min(row, a.n - 1) - rl * 16 - 4 * p;      // rows from the lane's own of the first blocks
-                            wv[i][e] = *reinterpret_cast<const uint32_t *>(c + 16 * e + w_at[i]);
-                            sv[i][e] = row < a.n ? scales[i][(int64_t)up * a.kg + s_at[i]] : (half_t)0.f;            // (rows past the last are no terms of the sum)
-                            zv[i][e] = zeros[i] ? (uint32_t)zeros[i][(int64_t)up * a.kg + s_at[i]] : (uint32_t)kGq4Sym;
-                        }
+                    int from = at;
+                    if constexpr (TRANS) {                                       // (blocks of rows past the last are not there)
+                        const int rl = (gw + i * (WR * WT)) & 3;
+                        from = (min((at >> 4) + rl, a.rb - 1) - rl) * 16;
                     }
+                    fetch_w(v, i, from);
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) put_w(i, h, own);
+                    for (int h = 0; h < 4; ++h) put_w(v, i, h, own, at, w);
                 }
             }
             __syncthreads();
@@ -361,18 +449,18 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_tile_kernel(Gq4TileA
         leave(a.y[0], a.y_ld[0], [&](int i, int t, int e) { return acc[i][t][e]; });
 }
 
-template <class T, int MODE, int SHIFT, int KG, int WR, int WT, int AF, int BF>
+template <class T, int MODE, int SHIFT, int KG, int P, int WR, int WT, int AF, int BF>
 static int launch_gq4_tile(Gq4TileArgs a, hipStream_t st)
 {
     constexpr int THREADS = KG * WR * WT * kWave, BO = 32 * AF * WR, BT = 32 * BF * WT;
-    constexpr size_t LDS = 2 * (size_t)KG * (BO + BT) * 128;
+    constexpr size_t LDS = Gq4TileLds<MODE, KG, BO, BT>::bytes;
     static_assert(LDS <= 160 * 1024 && (size_t)BO * BT * (KG > 1 ? 4 : 2) <= LDS, "LDS");
     const int outs = MODE == kGq4Transposed ? a.k : a.n, wide = MODE == kGq4Gated ? BO / 2 : BO;
     a.tiles_o = (int)(((int64_t)outs + wide - 1) / wide);
     a.tiles_t = (int)(((int64_t)a.m + BT - 1) / BT);
     const int64_t tiles = (int64_t)a.tiles_o * a.tiles_t;
     if (tiles * THREADS > UINT32_MAX) return SLIM_ERR_SHAPE;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(gq4_tile_kernel<T, MODE, SHIFT, KG, WR, WT, AF, BF>), dim3((unsigned)tiles), dim3(THREADS), LDS, st, a);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(gq4_tile_kernel<T, MODE, SHIFT, KG, P, WR, WT, AF, BF>), dim3((unsigned)tiles), dim3(THREADS), LDS, st, a);
     return SLIM_OK;
 }
 
@@ -382,12 +470,15 @@ static int launch_gq4_shape(const Gq4TileArgs &a, hipStream_t st)
     int shape = a.m > 256 ? 0 : 2;
     if (const char *e = getenv("GQ4_T")) shape = atoi(e);
     switch (shape) {
-    case 0: return launch_gq4_tile<T, MODE, SHIFT, 1, 4, 2, 2, 4>(a, st);     // 256 x 256
-    case 1: return launch_gq4_tile<T, MODE, SHIFT, 1, 4, 2, 2, 2>(a, st);     // 256 x 128
-    case 2: return launch_gq4_tile<T, MODE, SHIFT, 1, 2, 2, 2, 2>(a, st);     // 128 x 128
-    case 3: return launch_gq4_tile<T, MODE, SHIFT, 2, 2, 2, 2, 1>(a, st);     // 128 x 64, two groups
-    default: return launch_gq4_tile<T, MODE, SHIFT, 2, 2, 2, 2, 2>(a, st);    // 128 x 128, two groups
+    case 0: return launch_gq4_tile<T, MODE, SHIFT, 1, 1, 4, 2, 2, 4>(a, st);     // 256 x 256
+    case 1: return launch_gq4_tile<T, MODE, SHIFT, 1, 2, 4, 2, 2, 2>(a, st);     // 256 x 128
+    case 2: return launch_gq4_tile<T, MODE, SHIFT, 2, 2, 2, 2, 2, 2>(a, st);     // 128 x 128, two groups
+    case 3: return launch_gq4_tile<T, MODE, SHIFT, 2, 4, 2, 2, 2, 1>(a, st);     // 128 x 64, two groups
+    case 4: return launch_gq4_tile<T, MODE, SHIFT, 3, 3, 2, 1, 2, 1>(a, st);     // 128 x 32, three groups
+    default: break;
     }
+    if constexpr (MODE != kGq4Transposed) return launch_gq4_tile<T, MODE, SHIFT, 4, 3, 1, 2, 2, 1>(a, st);    // 64 x 64, four groups
+    return launch_gq4_tile<T, MODE, SHIFT, 3, 3, 2, 1, 2, 1>(a, st);
 }
 
 template <int MODE>
