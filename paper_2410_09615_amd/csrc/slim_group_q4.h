@@ -144,6 +144,18 @@ __device__ __forceinline__ float4_t gq4_mma16(Gq4Vec<BF16>::v8 a, Gq4Vec<BF16>::
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// The 16-byte pieces of an LDS row of 64 values are put in another order in each of eight rows, so that the lanes of a read or write find all banks; the
+// order is the same 32 rows on.
+__device__ __forceinline__ uint32_t gq4_turn(uint32_t row) { return (row & 7u) ^ (row >> 3 & 3u); }
+
+// A barrier for what is in LDS: unlike __syncthreads() it does not wait for loads that are under way to registers.
+__device__ __forceinline__ void gq4_lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+}
+
 // silu(g) = g sigma(g)
 __device__ __forceinline__ float gq4_sigma(float g) { return 1.f / (1.f + __expf(-g)); }
 

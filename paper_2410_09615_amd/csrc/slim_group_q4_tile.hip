@@ -25,23 +25,11 @@ struct Gq4TileArgs {
     int tiles_o, tiles_t;
 };
 
-// The 16-byte pieces of an LDS row of 64 values are put in another order in each of eight rows, so that the lanes of a read or write find all banks; the
-// order is the same 32 rows on.
-__device__ __forceinline__ uint32_t gq4_turn(uint32_t row) { return (row & 7u) ^ (row >> 3 & 3u); }
-
 // Per group of wavefronts: two buffers of a piece's weights and tokens, two windows of scales and zero points.
 template <int MODE, int KG, int BO, int BT>
 struct Gq4TileLds {
     static constexpr int table = MODE == kGq4Transposed ? 8 * 64 * 3 : BO * 24, bytes = KG * (2 * (BO + BT) * 128 + 2 * table);
 };
-
-// A barrier for what is in LDS: unlike __syncthreads() it does not wait for loads that are under way to registers.
-__device__ __forceinline__ void gq4_lds_barrier()
-{
-    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" : : : "memory");
-}
 
 // How the loop over the inputs is laid out.  KG groups of WR x WT wavefronts take turns at pieces of 64 inputs, each with two buffers of its own in LDS.  While a
 // piece is multiplied from one buffer, the next one goes from registers into the other, codes becoming numbers on the way, and the one after that is asked for from
@@ -500,6 +488,9 @@ static bool gq4_few(int m, int64_t x_ld) { return m <= kGq4Few && x_ld < (1 << 2
 int gq4_launch_stream(const slim_group_q4_layer *layer, const slim_group_q4_layer *up, int shift, const void *X, int64_t x_ld, int32_t m, void *const (&y)[3],
                       const int64_t (&y_ld)[3], int32_t dtype, hipStream_t st);
 
+int gq4_launch_rows(const slim_group_q4_layer *layer, const slim_group_q4_layer *up, int shift, const void *X, int64_t x_ld, int32_t m, void *const (&y)[3],
+                    const int64_t (&y_ld)[3], int32_t dtype, hipStream_t st);
+
 static Gq4TileArgs gq4_args(const slim_group_q4_layer *l, int shift, int m)
 {
     Gq4TileArgs a{};
@@ -542,7 +533,7 @@ extern "C" int slim_group_q4_gemm(const slim_group_q4_layer *layer, const void *
     a.y[0] = Y;
     a.y_ld[0] = y_ld;
     if (gq4_few(m, x_ld)) return gq4_launch_stream(layer, nullptr, shift, X, x_ld, m, a.y, a.y_ld, dtype, static_cast<hipStream_t>(stream));
-    return launch_gq4<kGq4Plain>(a, shift, dtype, static_cast<hipStream_t>(stream));
+    return gq4_launch_rows(layer, nullptr, shift, X, x_ld, m, a.y, a.y_ld, dtype, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int slim_group_q4_gemm_t(const slim_group_q4_layer *layer, const void *dY, int64_t dy_ld, int32_t m, void *dX, int64_t dx_ld, int32_t dtype,
@@ -582,7 +573,7 @@ extern "C" int slim_group_q4_gated(const slim_group_q4_layer *gate, const slim_g
     a.y[2] = U;
     a.y_ld[2] = u_ld;
     if (gq4_few(m, x_ld)) return gq4_launch_stream(gate, up, shift, X, x_ld, m, a.y, a.y_ld, dtype, static_cast<hipStream_t>(stream));
-    return launch_gq4<kGq4Gated>(a, shift, dtype, static_cast<hipStream_t>(stream));
+    return gq4_launch_rows(gate, up, shift, X, x_ld, m, a.y, a.y_ld, dtype, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int slim_group_q4_gated_backward(const slim_group_q4_layer *gate, const slim_group_q4_layer *up, const void *dH, int64_t dh_ld, const void *G,
