@@ -600,7 +600,7 @@ int slim_block_fp8_gemm_plan(int32_t n, int32_t k, int32_t m, int32_t dtype, int
  *   scales  fp16 [n][ceil(k / group)] and zeros uint8 of the same shape, row-major: as a checkpoint has them (slim_group_q4_sizes).
  * Scales that are not finite make the results that they are part of not finite; a zero point may be any byte.
  * Matrices of inputs and results may have any alignment of whole elements and a row stride (`_ld`, in elements, at least the row's length); codes are
- * 16-byte aligned.  k <= 2^22.  No call has a workspace, and none keeps anything.  Results do not depend on the order of workgroups.  All enqueue kernels
+ * 16-byte aligned.  k <= 2^22.  Nothing is kept between calls.  Results do not depend on the order of workgroups.  All enqueue kernels
  * only and may be captured into a HIP graph.
  */
 typedef struct {
@@ -626,14 +626,27 @@ int slim_group_q4_tile(const uint8_t *in, int64_t ld, int32_t n, int32_t k, uint
 int slim_group_q4_untile(const uint8_t *codes, int32_t n, int32_t k, uint8_t *out, int64_t ld, void *stream);
 int slim_group_q4_values(const slim_group_q4_layer *layer, void *out, int64_t ld, int32_t dtype, void *stream);
 
+/* The calls below, for slim_group_q4_workspace. */
+typedef enum { SLIM_GROUP_Q4_GEMM = 0, SLIM_GROUP_Q4_GATED = 1, SLIM_GROUP_Q4_GEMM_T = 2, SLIM_GROUP_Q4_GATED_BACKWARD = 3 } slim_group_q4_call;
+
+/*
+ * slim_group_q4_workspace -- bytes (HOST out-pointer) that a call on m tokens needs: 0 for many, among them up to 48 tokens forward; where there are fewer tiles of results than compute
+ * units, room for the sums of the workgroups that share a tile, in binary32.  Fewer tokens can need more.  The workspace is 16-byte aligned, need not be filled, and belongs to
+ * one call at a time: calls that may overlap (two streams, two graphs replayed side by side) have one each.  NULL where 0 bytes are needed.
+ * Errors: NULL, SHAPE.
+ */
+int slim_group_q4_workspace(int32_t n, int32_t k, int32_t m, int32_t call, size_t *bytes);
+
 /*
  * slim_group_q4_gemm   -- Y = X W^T:  X [m][k], Y [m][n] of `dtype` (SLIM_F16, SLIM_BF16), any m >= 1.
  * slim_group_q4_gemm_t -- dX = dY W:  the gradient of X through frozen weights; dY [m][n], dX [m][k].
  * Sums in binary32, one rounding of each result.
- * X, Y (dY, dX) do not overlap.  Errors: NULL, SHAPE, ALIGN, HIP.
+ * X, Y (dY, dX) do not overlap.  Errors: NULL, SHAPE, ALIGN, WORKSPACE, HIP.
  */
-int slim_group_q4_gemm(const slim_group_q4_layer *layer, const void *X, int64_t x_ld, int32_t m, void *Y, int64_t y_ld, int32_t dtype, void *stream);
-int slim_group_q4_gemm_t(const slim_group_q4_layer *layer, const void *dY, int64_t dy_ld, int32_t m, void *dX, int64_t dx_ld, int32_t dtype, void *stream);
+int slim_group_q4_gemm(const slim_group_q4_layer *layer, const void *X, int64_t x_ld, int32_t m, void *Y, int64_t y_ld, int32_t dtype, void *workspace,
+                       size_t workspace_bytes, void *stream);
+int slim_group_q4_gemm_t(const slim_group_q4_layer *layer, const void *dY, int64_t dy_ld, int32_t m, void *dX, int64_t dx_ld, int32_t dtype, void *workspace,
+                         size_t workspace_bytes, void *stream);
 
 /*
  * slim_group_q4_gated -- the first half of a gated feed-forward block in one kernel:
@@ -644,13 +657,13 @@ int slim_group_q4_gemm_t(const slim_group_q4_layer *layer, const void *dY, int64
  *   dU = dH silu(G),  dG = dH U sigma(G) (1 + G (1 - sigma(G))),  dX = dG Wg + dU Wu,
  * all of `dtype`; dG and dU [m][n] (what a low-rank term beside the layers needs) are rounded once, and dX is the product of the rounded ones.
  * dG may be G or dH, dU may be U or dH (same pointer and stride), not both the same; no other overlap.
- * Errors: NULL, SHAPE (the two layers' sizes too), ALIGN, HIP.
+ * Errors: NULL, SHAPE (the two layers' sizes too), ALIGN, WORKSPACE, HIP.
  */
 int slim_group_q4_gated(const slim_group_q4_layer *gate, const slim_group_q4_layer *up, const void *X, int64_t x_ld, int32_t m, void *H, int64_t h_ld, void *G,
-                        int64_t g_ld, void *U, int64_t u_ld, int32_t dtype, void *stream);
+                        int64_t g_ld, void *U, int64_t u_ld, int32_t dtype, void *workspace, size_t workspace_bytes, void *stream);
 int slim_group_q4_gated_backward(const slim_group_q4_layer *gate, const slim_group_q4_layer *up, const void *dH, int64_t dh_ld, const void *G, int64_t g_ld,
                                  const void *U, int64_t u_ld, int32_t m, void *dG, int64_t dg_ld, void *dU, int64_t du_ld, void *dX, int64_t dx_ld,
-                                 int32_t dtype, void *stream);
+                                 int32_t dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Measurement aids (they compute nothing of the method): what this machine

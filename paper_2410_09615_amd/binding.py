@@ -56,7 +56,7 @@ EXPORTS = ["slim_status_string", "slim_rank_pad", "slim_packed_sizes", "slim_pac
            "slim_block_fp8_tile", "slim_block_fp8_untile", "slim_block_fp8_gemm_workspace", "slim_block_fp8_gemm",
            "slim_block_fp8_gemm_plan",
            "slim_group_q4_sizes", "slim_group_q4_weight", "slim_group_q4_tile", "slim_group_q4_untile", "slim_group_q4_values", "slim_group_q4_gemm",
-           "slim_group_q4_gemm_t", "slim_group_q4_gated", "slim_group_q4_gated_backward"]
+           "slim_group_q4_gemm_t", "slim_group_q4_gated", "slim_group_q4_gated_backward", "slim_group_q4_workspace"]
 
 
 def lib():
@@ -117,9 +117,10 @@ def lib():
         L.slim_group_q4_tile.argtypes = [vp, i64, i32, i32, vp, vp]
         L.slim_group_q4_untile.argtypes = [vp, i32, i32, vp, i64, vp]
         L.slim_group_q4_values.argtypes = [pq4, vp, i64, i32, vp]
-        L.slim_group_q4_gemm.argtypes = L.slim_group_q4_gemm_t.argtypes = [pq4, vp, i64, i32, vp, i64, i32, vp]
-        L.slim_group_q4_gated.argtypes = [pq4, pq4, vp, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp]
-        L.slim_group_q4_gated_backward.argtypes = [pq4, pq4, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp]
+        L.slim_group_q4_workspace.argtypes = [i32, i32, i32, i32, psz]
+        L.slim_group_q4_gemm.argtypes = L.slim_group_q4_gemm_t.argtypes = [pq4, vp, i64, i32, vp, i64, i32, vp, sz, vp]
+        L.slim_group_q4_gated.argtypes = [pq4, pq4, vp, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp, sz, vp]
+        L.slim_group_q4_gated_backward.argtypes = [pq4, pq4, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp, sz, vp]
         for name in EXPORTS[2:]:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -935,39 +936,57 @@ def slim_group_q4_values(layer: SlimGroupQ4Weight, dtype: torch.dtype = torch.fl
     return values
 
 
-def _q4_call(name: str, device: int, call):
-    """call(again) until it has been enqueued: once more with the layers' references made anew, or with the tensors' device current."""
-    status = call(False)
+Q4_CALLS = {"gemm": 0, "gated": 1, "gemm_t": 2, "gated_backward": 3}
+
+
+def slim_group_q4_workspace(n: int, k: int, m: int, call: str = "gemm") -> int:
+    """Bytes that a call ("gemm", "gated", "gemm_t", "gated_backward") on m tokens needs; fewer tokens can need more."""
+    out = ctypes.c_size_t()
+    _check("slim_group_q4_workspace", lib().slim_group_q4_workspace(n, k, m, Q4_CALLS[call], out))
+    return out.value
+
+
+def alloc_group_q4_workspace(layer: SlimGroupQ4Weight, m: int, call: str = "gemm") -> torch.Tensor:
+    """A workspace for `call` on m tokens, not filled; it belongs to one call at a time."""
+    return torch.empty(slim_group_q4_workspace(layer.n, layer.k, m, call), dtype=torch.uint8, device=layer.codes.device)
+
+
+def _q4_call(name: str, layer: SlimGroupQ4Weight, device: int, m: int, workspace, status: int, call) -> None:
+    """call(again, workspace) until it has been enqueued, after it returned `status`: with the layers' references made anew, with the tensors' device current, with
+    a workspace of its own where none was given."""
     if status == 1:                                   # a layer's tensors have other data than its reference says
-        status = call(True)
+        status = call(True, workspace)
     if status == 2:                                   # another device is current
         with torch.cuda.device(device):
-            status = call(False)
+            return _q4_call(name, layer, device, m, workspace, call(False, workspace), call)
+    if status == SLIM_ERR_WORKSPACE and workspace is None:
+        status = call(False, alloc_group_q4_workspace(layer, m, name.removeprefix("slim_group_q4_")))
     if status != SLIM_OK:
         _check(name, status)
 
 
-def _q4_product(name: str, transposed: bool, layer: SlimGroupQ4Weight, X: torch.Tensor, Y) -> torch.Tensor:
+def _q4_product(name: str, transposed: bool, layer: SlimGroupQ4Weight, X: torch.Tensor, Y, workspace) -> torch.Tensor:
     ref = layer.c_ref()
     if Y is None:
         Y = torch.empty(X.shape[0], layer.k if transposed else layer.n, dtype=X.dtype, device=layer.codes.device)
-    status = (_call or _calls()).q4_product(transposed, ref.address, ref.device, layer.codes, layer.scales, layer.zeros, X, Y)
+    status = (_call or _calls()).q4_product(transposed, ref.address, ref.device, layer.codes, layer.scales, layer.zeros, X, Y, workspace)
     if status != SLIM_OK:
-        def call(again):
+        def call(again, ws):
             r = layer.c_ref(again)
-            return _call.q4_product(transposed, r.address, r.device, layer.codes, layer.scales, layer.zeros, X, Y)
-        _q4_call(name, ref.device, call)
+            return _call.q4_product(transposed, r.address, r.device, layer.codes, layer.scales, layer.zeros, X, Y, ws)
+        _q4_call(name, layer, ref.device, X.shape[0], workspace, status, call)
     return Y
 
 
-def slim_group_q4_gemm(layer: SlimGroupQ4Weight, X: torch.Tensor, Y=None) -> torch.Tensor:
-    """Y [m][n] = X W^T; X fp16 or bf16 [m][k], Y of its type (None: a new one), any row strides, any m >= 1."""
-    return _q4_product("slim_group_q4_gemm", False, layer, X, Y)
+def slim_group_q4_gemm(layer: SlimGroupQ4Weight, X: torch.Tensor, Y=None, workspace=None) -> torch.Tensor:
+    """Y [m][n] = X W^T; X fp16 or bf16 [m][k], Y of its type (None: a new one), any row strides, any m >= 1.
+    workspace: alloc_group_q4_workspace's, or None for one of the call's own where it needs any."""
+    return _q4_product("slim_group_q4_gemm", False, layer, X, Y, workspace)
 
 
-def slim_group_q4_gemm_t(layer: SlimGroupQ4Weight, dY: torch.Tensor, dX=None) -> torch.Tensor:
+def slim_group_q4_gemm_t(layer: SlimGroupQ4Weight, dY: torch.Tensor, dX=None, workspace=None) -> torch.Tensor:
     """dX [m][k] = dY W: the gradient of the product's input (the weights are frozen); dY fp16 or bf16 [m][n], dX of its type."""
-    return _q4_product("slim_group_q4_gemm_t", True, layer, dY, dX)
+    return _q4_product("slim_group_q4_gemm_t", True, layer, dY, dX, workspace)
 
 
 def _q4_pair(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight, again: bool):
@@ -975,28 +994,30 @@ def _q4_pair(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight, again: bool):
     return g.address, g.device, gate.codes, gate.scales, gate.zeros, u.address, u.device, up.codes, up.scales, up.zeros
 
 
-def slim_group_q4_gated(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight, X: torch.Tensor, H=None, G=None, U=None):
+def slim_group_q4_gated(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight, X: torch.Tensor, H=None, G=None, U=None, workspace=None):
     """H [m][n] = silu(X Wg^T) * (X Wu^T) -> (H, G, U).  G, U: True for a new matrix that receives the two products (what
     slim_group_q4_gated_backward wants), or one to write; None (returned as such): not wanted.  All of X's type, any row strides, any m >= 1."""
     ref = gate.c_ref()
     if H is None or G is True or U is True:
         new = lambda: torch.empty(X.shape[0], gate.n, dtype=X.dtype, device=gate.codes.device)
         H, G, U = new() if H is None else H, new() if G is True else G, new() if U is True else U
-    status = (_call or _calls()).q4_gated(*_q4_pair(gate, up, False), X, H, G, U)
+    status = (_call or _calls()).q4_gated(*_q4_pair(gate, up, False), X, H, G, U, workspace)
     if status != SLIM_OK:
-        _q4_call("slim_group_q4_gated", ref.device, lambda again: _call.q4_gated(*_q4_pair(gate, up, again), X, H, G, U))
+        _q4_call("slim_group_q4_gated", gate, ref.device, X.shape[0], workspace, status,
+                 lambda again, ws: _call.q4_gated(*_q4_pair(gate, up, again), X, H, G, U, ws))
     return H, G, U
 
 
 def slim_group_q4_gated_backward(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight, dH: torch.Tensor, G: torch.Tensor, U: torch.Tensor, dG=None, dU=None,
-                                 dX=None):
+                                 dX=None, workspace=None):
     """Gradients through slim_group_q4_gated, its weights frozen: dH, G, U [m][n] -> (dX [m][k], dG [m][n], dU [m][n]), all of one type.
     dG may be G or dH and dU may be U or dH, but not both the same."""
     ref = gate.c_ref()
     if dG is None or dU is None or dX is None:
         new = lambda k: torch.empty(dH.shape[0], k, dtype=dH.dtype, device=gate.codes.device)
         dG, dU, dX = new(gate.n) if dG is None else dG, new(gate.n) if dU is None else dU, new(gate.k) if dX is None else dX
-    status = (_call or _calls()).q4_backward(*_q4_pair(gate, up, False), dH, G, U, dG, dU, dX)
+    status = (_call or _calls()).q4_backward(*_q4_pair(gate, up, False), dH, G, U, dG, dU, dX, workspace)
     if status != SLIM_OK:
-        _q4_call("slim_group_q4_gated_backward", ref.device, lambda again: _call.q4_backward(*_q4_pair(gate, up, again), dH, G, U, dG, dU, dX))
+        _q4_call("slim_group_q4_gated_backward", gate, ref.device, dH.shape[0], workspace, status,
+                 lambda again, ws: _call.q4_backward(*_q4_pair(gate, up, again), dH, G, U, dG, dU, dX, ws))
     return dX, dG, dU

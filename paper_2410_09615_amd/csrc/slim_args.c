@@ -21,12 +21,12 @@ static int (*call_act)(const void *, int64_t, const void *, int64_t, int32_t, in
 static int (*call_gemm)(const slim_block_fp8_layer *, const uint8_t *, const float *, int32_t, void *, int64_t, int32_t, void *, size_t,
                         void *);
 
-typedef int (*q4_product_call)(const slim_group_q4_layer *, const void *, int64_t, int32_t, void *, int64_t, int32_t, void *);
+typedef int (*q4_product_call)(const slim_group_q4_layer *, const void *, int64_t, int32_t, void *, int64_t, int32_t, void *, size_t, void *);
 static q4_product_call call_q4_gemm, call_q4_gemm_t;
 static int (*call_q4_gated)(const slim_group_q4_layer *, const slim_group_q4_layer *, const void *, int64_t, int32_t, void *, int64_t, void *, int64_t, void *,
-                            int64_t, int32_t, void *);
+                            int64_t, int32_t, void *, size_t, void *);
 static int (*call_q4_backward)(const slim_group_q4_layer *, const slim_group_q4_layer *, const void *, int64_t, const void *, int64_t, const void *, int64_t,
-                               int32_t, void *, int64_t, void *, int64_t, void *, int64_t, int32_t, void *);
+                               int32_t, void *, int64_t, void *, int64_t, void *, int64_t, int32_t, void *, size_t, void *);
 
 static int refuse(const char *name, const char *why)
 {
@@ -249,6 +249,16 @@ static int q4_matrix(PyObject *t, const char *name, long long m, long long k, in
     return 0;
 }
 
+/* A workspace, or None: no bytes. */
+static int q4_room(PyObject *t, long long device, void **p, long long *bytes)
+{
+    *p = NULL;
+    *bytes = 0;
+    if (t == Py_None) return 0;
+    *bytes = number(t, s_numel);
+    return *bytes < 0 || whole(t, "workspace", U8, U8, *bytes, device, p) ? -1 : 0;
+}
+
 /* 1 where the device is not the current one, -1 with an exception set. */
 static int elsewhere(long long device)
 {
@@ -259,65 +269,65 @@ static int elsewhere(long long device)
     return PyErr_Occurred() ? -1 : now != device;
 }
 
-/* q4_product(transposed, layer (5), X, Y) */
+/* q4_product(transposed, layer (5), X, Y, workspace) */
 static PyObject *q4_product(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
     (void)self;
-    if (n != 8) return PyErr_Format(PyExc_TypeError, "q4_product takes 8 arguments");
-    long long device;
+    if (n != 9) return PyErr_Format(PyExc_TypeError, "q4_product takes 9 arguments");
+    long long device, room;
     int stale = 0, status;
     const int transposed = a[0] == Py_True;
     const slim_group_q4_layer *l = q4_layer(a + 1, &device, &stale);
     if (!l) return NULL;
     if (stale) return PyLong_FromLong(STALE);
     matrix x, y;
-    void *st;
+    void *st, *ws;
     if (q4_matrix(a[6], transposed ? "dY" : "X", -1, transposed ? l->n : l->k, -1, device, &x) ||
-        q4_matrix(a[7], transposed ? "dX" : "Y", x.m, transposed ? l->k : l->n, x.type, device, &y))
+        q4_matrix(a[7], transposed ? "dX" : "Y", x.m, transposed ? l->k : l->n, x.type, device, &y) || q4_room(a[8], device, &ws, &room))
         return NULL;
     const int away = elsewhere(device);
     if (away < 0) return NULL;
     if (away) return PyLong_FromLong(ELSEWHERE);
     if (stream(device, &st)) return NULL;
     Py_BEGIN_ALLOW_THREADS
-    status = (transposed ? call_q4_gemm_t : call_q4_gemm)(l, x.p, x.ld, (int32_t)x.m, y.p, y.ld, x.type, st);
+    status = (transposed ? call_q4_gemm_t : call_q4_gemm)(l, x.p, x.ld, (int32_t)x.m, y.p, y.ld, x.type, ws, (size_t)room, st);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(status);
 }
 
-/* q4_gated(gate (5), up (5), X, H, G, U); G, U may be None */
+/* q4_gated(gate (5), up (5), X, H, G, U, workspace); G, U, workspace may be None */
 static PyObject *q4_gated(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
     (void)self;
-    if (n != 14) return PyErr_Format(PyExc_TypeError, "q4_gated takes 14 arguments");
-    long long device, other;
+    if (n != 15) return PyErr_Format(PyExc_TypeError, "q4_gated takes 15 arguments");
+    long long device, other, room;
     int stale = 0, status;
     const slim_group_q4_layer *gate = q4_layer(a, &device, &stale), *up = gate ? q4_layer(a + 5, &other, &stale) : NULL;
     if (!up) return NULL;
     if (stale) return PyLong_FromLong(STALE);
     if (other != device) return refuse("up", "must be on gate's device"), NULL;
     matrix x, h, g = {0}, u = {0};
-    void *st;
+    void *st, *ws;
     if (q4_matrix(a[10], "X", -1, gate->k, -1, device, &x) || q4_matrix(a[11], "H", x.m, gate->n, x.type, device, &h) ||
         (a[12] != Py_None && q4_matrix(a[12], "G", x.m, gate->n, x.type, device, &g)) ||
-        (a[13] != Py_None && q4_matrix(a[13], "U", x.m, gate->n, x.type, device, &u)))
+        (a[13] != Py_None && q4_matrix(a[13], "U", x.m, gate->n, x.type, device, &u)) || q4_room(a[14], device, &ws, &room))
         return NULL;
     const int away = elsewhere(device);
     if (away < 0) return NULL;
     if (away) return PyLong_FromLong(ELSEWHERE);
     if (stream(device, &st)) return NULL;
     Py_BEGIN_ALLOW_THREADS
-    status = call_q4_gated(gate, up, x.p, x.ld, (int32_t)x.m, h.p, h.ld, g.p, g.ld, u.p, u.ld, x.type, st);
+    status = call_q4_gated(gate, up, x.p, x.ld, (int32_t)x.m, h.p, h.ld, g.p, g.ld, u.p, u.ld, x.type, ws, (size_t)room, st);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(status);
 }
 
-/* q4_backward(gate (5), up (5), dH, G, U, dG, dU, dX) */
+/* q4_backward(gate (5), up (5), dH, G, U, dG, dU, dX, workspace) */
 static PyObject *q4_backward(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
     (void)self;
-    if (n != 16) return PyErr_Format(PyExc_TypeError, "q4_backward takes 16 arguments");
-    long long device, other;
+    if (n != 17) return PyErr_Format(PyExc_TypeError, "q4_backward takes 17 arguments");
+    long long device, other, room;
     int stale = 0, status;
     const slim_group_q4_layer *gate = q4_layer(a, &device, &stale), *up = gate ? q4_layer(a + 5, &other, &stale) : NULL;
     if (!up) return NULL;
@@ -325,16 +335,17 @@ static PyObject *q4_backward(PyObject *self, PyObject *const *a, Py_ssize_t n)
     if (other != device) return refuse("up", "must be on gate's device"), NULL;
     static const char *const names[] = {"dH", "G", "U", "dG", "dU", "dX"};
     matrix v[6];
-    void *st;
+    void *st, *ws;
     for (int i = 0; i < 6; ++i)
         if (q4_matrix(a[10 + i], names[i], i ? v[0].m : -1, i < 5 ? gate->n : gate->k, i ? v[0].type : -1, device, &v[i])) return NULL;
+    if (q4_room(a[16], device, &ws, &room)) return NULL;
     const int away = elsewhere(device);
     if (away < 0) return NULL;
     if (away) return PyLong_FromLong(ELSEWHERE);
     if (stream(device, &st)) return NULL;
     Py_BEGIN_ALLOW_THREADS
     status = call_q4_backward(gate, up, v[0].p, v[0].ld, v[1].p, v[1].ld, v[2].p, v[2].ld, (int32_t)v[0].m, v[3].p, v[3].ld, v[4].p, v[4].ld, v[5].p, v[5].ld,
-                              v[0].type, st);
+                              v[0].type, ws, (size_t)room, st);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(status);
 }

@@ -10,7 +10,8 @@ namespace slim {
 // lane holds of the four 16 x 16 x 32 products over the block's inputs: its dword j has inputs 32 j + 8 q .. + 7 of row r.  Inputs 2 i and
 // 2 i + 1 of a dword are its nibbles i and i + 4, so that shifting by 4 i and masking leaves the two as 16-bit halves.
 constexpr int kGq4Rows = 16, kGq4Cols = 128, kGq4Block = 1024;
-constexpr int kGq4Few = 48;                   // tokens up to which weights are streamed
+// Whether weights are streamed (slim_group_q4_stream.hip): up to 48 tokens.
+inline bool gq4_streamed(int n, int m, bool gated) { return m <= 48; }
 constexpr int kGq4Sym = 8;                    // the zero point of symmetric weights
 
 inline int gq4_row_blocks(int n) { return (int)(((int64_t)n + kGq4Rows - 1) / kGq4Rows); }
@@ -155,6 +156,51 @@ __device__ __forceinline__ void gq4_lds_barrier()
     __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
 }
+
+// ---- products whose inputs are shared by several workgroups ----
+// Where there are fewer tiles than compute units, `splits` workgroups take a share each of what a tile sums over, and leave their sums in binary32: part[split][m][ld], of a gated block G's
+// and then U's, 2 m rows.  gq4_launch_finish adds them in order and rounds.
+struct Gq4Split {
+    float *part;             // null: one workgroup has it all
+    int splits, ld;
+};
+constexpr int kGq4Reads = 4 << 20;           // bytes that the memory system moves in about a microsecond
+inline int gq4_part_ld(int outs) { return (int)(((int64_t)outs + 7) / 8 * 8); }
+inline int64_t gq4_part_bytes(int splits, int m, int outs, bool gated) { return splits > 1 ? (int64_t)splits * m * gq4_part_ld(outs) * (gated ? 8 : 4) : 0; }
+
+// A tile's shape: outputs and tokens, workgroups to a compute unit, the time (us) of a step of 64 inputs with few and with all compute units at work.
+struct Gq4Shape {
+    int outs, toks, per_cu;
+    float few, all;
+};
+struct Gq4Plan {
+    int shape, splits;
+};
+// The shape and number of splits with the least of rounds x (steps x time + 4 us) and what sums left in memory cost.
+template <int N>
+inline Gq4Plan gq4_plan(const Gq4Shape (&shapes)[N], int outs, int m, int steps, bool gated)
+{
+    const double cus = device_info().cus;
+    Gq4Plan best{0, 1};
+    double least = 0;
+    for (int i = 0; i < N; ++i) {
+        const Gq4Shape &s = shapes[i];
+        const double tiles = (double)(((int64_t)outs * (gated ? 2 : 1) + s.outs - 1) / s.outs) * (double)(((int64_t)m + s.toks - 1) / s.toks);
+        for (int splits = 1; splits <= 16 && (splits == 1 || (tiles * splits <= cus * s.per_cu && splits * 8 <= steps)); ++splits) {
+            const double slots = cus * s.per_cu, rounds = __builtin_ceil(tiles * splits / slots), busy = tiles * splits / cus;
+            const double step = busy <= 0.5 ? s.few : busy >= 1 ? s.all : s.few + (s.all - s.few) * (busy - 0.5) * 2;
+            double time = rounds * (((steps + splits - 1) / splits) * step + 4);
+            if (splits > 1) time += 4 + (2.0 * (double)gq4_part_bytes(splits, m, outs, gated) + 2.0 * m * outs) / kGq4Reads;
+            if ((i == 0 && splits == 1) || time < least) {
+                least = time;
+                best = Gq4Plan{i, splits};
+            }
+        }
+    }
+    return best;
+}
+
+int gq4_launch_finish(const Gq4Split &p, int m, int outs, bool gated, void *const (&y)[3], const int64_t (&y_ld)[3], int32_t dtype, hipStream_t st);
 
 // silu(g) = g sigma(g)
 __device__ __forceinline__ float gq4_sigma(float g) { return 1.f / (1.f + __expf(-g)); }

@@ -7,6 +7,8 @@
 // Quotients in binary32.  The scale is rounded to fp16 before the codes are made, so codes are the nearest ones to the scale that is kept.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "slim_group_q4.h"
 
 namespace slim {
@@ -176,6 +178,58 @@ __global__ __launch_bounds__(256) void gq4_act_backward_kernel(Gq4ActArgs a)
         store_piece<T, 8>(static_cast<E *>(a.dG) + row * a.dg_ld, at, a.n, u);
         store_piece<T, 8>(static_cast<E *>(a.dU) + row * a.du_ld, at, a.n, h);
     }
+}
+
+// Sums of several workgroups, added in order; a thread has 8 of a token's results at a time.
+template <class T, bool GATED>
+__global__ __launch_bounds__(256) void gq4_finish_kernel(Gq4Split p, int m, int outs, int64_t pieces, void *y0, void *y1, void *y2, int64_t ld0, int64_t ld1, int64_t ld2)
+{
+    typedef typename T::type E;
+    const int per_row = p.ld / 8;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / per_row;
+        const int at = (int)(i % per_row) * 8;
+        float v[GATED ? 2 : 1][8];
+#pragma unroll
+        for (int u = 0; u < (GATED ? 2 : 1); ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
+        for (int z = 0; z < p.splits; ++z)
+#pragma unroll
+            for (int u = 0; u < (GATED ? 2 : 1); ++u) {
+                const float4_t *q = reinterpret_cast<const float4_t *>(p.part + (((int64_t)z * (GATED ? 2 : 1) + u) * m + row) * p.ld + at);
+                const float4_t a = q[0], b = q[1];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[u][e] += a[e];
+                    v[u][4 + e] += b[e];
+                }
+            }
+        if constexpr (GATED) {
+            float h[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[e] = v[0][e] * gq4_sigma(v[0][e]) * v[1][e];
+            store_piece<T, 8>(static_cast<E *>(y0) + row * ld0, at, outs, h);
+            if (y1) store_piece<T, 8>(static_cast<E *>(y1) + row * ld1, at, outs, v[0]);
+            if (y2) store_piece<T, 8>(static_cast<E *>(y2) + row * ld2, at, outs, v[1]);
+        } else
+            store_piece<T, 8>(static_cast<E *>(y0) + row * ld0, at, outs, v[0]);
+    }
+}
+
+int gq4_launch_finish(const Gq4Split &p, int m, int outs, bool gated, void *const (&y)[3], const int64_t (&y_ld)[3], int32_t dtype, hipStream_t st)
+{
+    const int64_t pieces = (int64_t)m * (p.ld / 8), groups = (pieces + 255) / 256;
+    const dim3 grid((unsigned)(groups < 8192 ? groups : 8192)), threads(256);
+    auto launch = [&](auto type, auto g) {
+        hipLaunchKernelGGL(HIP_KERNEL_NAME(gq4_finish_kernel<decltype(type), decltype(g)::value>), grid, threads, 0, st, p, m, outs, pieces, y[0], y[1], y[2], y_ld[0],
+                           y_ld[1], y_ld[2]);
+    };
+    if (dtype == SLIM_F16)
+        gated ? launch(F16{}, std::true_type{}) : launch(F16{}, std::false_type{});
+    else
+        gated ? launch(BF16{}, std::true_type{}) : launch(BF16{}, std::false_type{});
+    return hip_status(hipGetLastError());
 }
 
 template <class T, bool ZEROS>

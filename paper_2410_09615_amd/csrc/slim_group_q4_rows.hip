@@ -11,6 +11,17 @@
 
 namespace slim {
 
+constexpr Gq4Shape kRowShapes[] = {{256, 256, 1, 1.24f, 1.94f}, {256, 128, 2, 0.88f, 1.0f}, {256, 64, 1, 0.55f, 0.65f}, {128, 64, 1, 0.38f, 0.5f}};
+
+static Gq4Plan gq4_plan_rows(int n, int k, int m, bool gated)
+{
+    Gq4Plan p = gq4_plan(kRowShapes, n, m, 2 * (k / kGq4Cols), gated);
+    if (const char *e = getenv("GQ4_F")) p.shape = atoi(e);
+    if (const char *e = getenv("GQ4_Z")) p.splits = atoi(e);
+    return p;
+}
+int64_t gq4_rows_workspace(int n, int k, int m, bool gated) { return gq4_part_bytes(gq4_plan_rows(n, k, m, gated).splits, m, n, gated); }
+
 struct Gq4RowsArgs {
     Gq4Weights w[2];
     const void *x;
@@ -19,6 +30,7 @@ struct Gq4RowsArgs {
     int64_t y_ld[3];
     int n, k, m, cb, rb, kg; // the layer: rows, inputs; blocks of inputs, blocks of rows, groups of a row
     int tiles_o, tiles_t;
+    Gq4Split split;
 };
 
 // Per group of wavefronts: two buffers of a step's tokens, two windows of scales and zero points (8 groups of each row).
@@ -48,7 +60,9 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
     const int qx = gx % kDies == 0 ? ((int)blockIdx.x % kDies) * (gx / kDies) + (int)blockIdx.x / kDies : (int)blockIdx.x;
     const int tile = blocked_tile(qx, a.tiles_o, a.tiles_t);
     const int o0 = tile % a.tiles_o * (GATED ? BO / 2 : BO), t0 = tile / a.tiles_o * BT, outs = a.n;
-    const int whole = a.k / kGq4Cols, steps = 2 * whole, turns = (steps + KG - 1) / KG, first = group * turns, last = max(min(first + turns, steps) - 1, 0);
+    // this workgroup's share of the steps, and its groups' of that
+    const int whole = a.k / kGq4Cols, share = (2 * whole + a.split.splits - 1) / a.split.splits, begin = (int)blockIdx.y * share, end = min(begin + share, 2 * whole);
+    const int steps = end - begin, turns = (steps + KG - 1) / KG, first = begin + group * turns, last = max(min(first + turns, end) - 1, 0);
     uint8_t *const own = lds + group * (2 * STAGE + 2 * TABLE), *const tables = own + 2 * STAGE;
 
     // ---- weights: lane (half, row of 32) of row tile i ----
@@ -190,7 +204,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
         Codes w[RW];
         Tokens x[RX];
         auto step_of = [&](int s) { return min(first + s, last); };
-        const int mine = min(turns, steps - first);
+        const int mine = min(turns, end - first);
         int window = window_of(step_of(0));
         load_window(window);
 #pragma unroll
@@ -257,7 +271,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
             }
         }
     }
-    if (whole < a.cb) {
+    if (whole < a.cb && (int)blockIdx.y == a.split.splits - 1) {
         // inputs that end inside a block: its two halves, tokens element by element, without overlap
         const int left = a.k - whole * kGq4Cols, w = window_of(2 * whole);
         load_window(w);
@@ -312,6 +326,24 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
         }
     }
 
+    // (uniform: all of a workgroup or none)
+    if (a.split.part) {
+        if (KG == 1 || group == 0)
+#pragma unroll
+            for (int i = 0; i < AF; ++i)
+#pragma unroll
+                for (int t = 0; t < BF; ++t) {
+                    const int tok = t0 + (wt * BF + t) * 32 + (lane & 31), o = o0 + (GATED ? (wr * AF + i) / 2 : wr * AF + i) * 32 + 4 * (lane >> 5);
+                    float *const row = a.split.part + (((int64_t)blockIdx.y * (GATED ? 2 : 1) + (GATED ? i & 1 : 0)) * a.m + tok) * a.split.ld + o;
+                    if (tok < a.m)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g)
+                            if (o + 8 * g < a.split.ld)
+                                *reinterpret_cast<float4_t *>(row + 8 * g) = float4_t{acc[i][t][4 * g], acc[i][t][4 * g + 1], acc[i][t][4 * g + 2], acc[i][t][4 * g + 3]};
+                }
+        return;
+    }
+
     // Results leave through LDS, so that a store writes whole pieces of a token's row.
     constexpr int OUT = GATED ? BO / 2 : BO, PER_ROW = OUT / 8, TURN = (PER_ROW < 16 ? PER_ROW : 16) - 1;
     typedef E vec4 __attribute__((ext_vector_type(4)));
@@ -358,42 +390,40 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
         leave(a.y[0], a.y_ld[0], [&](int i, int t, int e) { return acc[i][t][e]; });
 }
 
-template <class T, bool GATED, int SHIFT, int KG, int WR, int WT, int BF, int RX, int RW>
+template <class T, bool GATED, int SHIFT, int SHAPE, int KG, int WR, int WT, int BF, int RX, int RW>
 static int launch_gq4_rows_of(Gq4RowsArgs a, hipStream_t st)
 {
     constexpr int THREADS = KG * WR * WT * kWave, BO = 64 * WR, BT = 32 * BF * WT;
     constexpr size_t OUT = (size_t)BO * BT * 2 / (GATED ? 2 : 1), SUMS = KG > 1 ? (size_t)BO * BT * 4 : 0, RING = Gq4RowsLds<KG, BO, BT>::bytes;
     constexpr size_t LDS = RING > OUT ? (RING > SUMS ? RING : SUMS) : OUT > SUMS ? OUT : SUMS;
-    static_assert(LDS <= 160 * 1024, "LDS");
+    static_assert(LDS * kRowShapes[SHAPE].per_cu <= 160 * 1024 && kRowShapes[SHAPE].outs == BO && kRowShapes[SHAPE].toks == BT, "the table's tile");
     const int wide = GATED ? BO / 2 : BO;
     a.tiles_o = (int)(((int64_t)a.n + wide - 1) / wide);
     a.tiles_t = (int)(((int64_t)a.m + BT - 1) / BT);
     const int64_t tiles = (int64_t)a.tiles_o * a.tiles_t;
     if (tiles * THREADS > UINT32_MAX) return SLIM_ERR_SHAPE;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(gq4_rows_kernel<T, GATED, SHIFT, KG, WR, WT, BF, RX, RW>), dim3((unsigned)tiles), dim3(THREADS), LDS, st, a);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(gq4_rows_kernel<T, GATED, SHIFT, KG, WR, WT, BF, RX, RW>), dim3((unsigned)tiles, (unsigned)a.split.splits), dim3(THREADS), LDS, st, a);
     return SLIM_OK;
 }
 
 template <class T, bool GATED, int SHIFT>
-static int launch_gq4_rows_shape(const Gq4RowsArgs &a, hipStream_t st)
+static int launch_gq4_rows_shape(const Gq4RowsArgs &a, int shape, hipStream_t st)
 {
-    int shape = a.m > 256 ? 0 : 2;
-    if (const char *e = getenv("GQ4_F")) shape = atoi(e);
     switch (shape) {
-    case 0: return launch_gq4_rows_of<T, GATED, SHIFT, 1, 4, 2, 4, 1, 2>(a, st);     // 256 rows x 256 tokens
-    case 1: return launch_gq4_rows_of<T, GATED, SHIFT, 1, 4, 1, 4, 1, 2>(a, st);     // 256 x 128, 4 wavefronts
-    case 2: return launch_gq4_rows_of<T, GATED, SHIFT, 2, 4, 1, 2, 2, 2>(a, st);     // 256 x 64, two groups
-    case 3: return launch_gq4_rows_of<T, GATED, SHIFT, 4, 2, 1, 2, 2, 2>(a, st);     // 128 x 64, four groups
-    case 4: return launch_gq4_rows_of<T, GATED, SHIFT, 8, 1, 1, 2, 2, 2>(a, st);     // 64 x 64, eight groups
-    default: return launch_gq4_rows_of<T, GATED, SHIFT, 2, 2, 1, 4, 1, 2>(a, st);    // 128 x 128, two groups
+    case 0: return launch_gq4_rows_of<T, GATED, SHIFT, 0, 1, 4, 2, 4, 1, 2>(a, st);
+    case 1: return launch_gq4_rows_of<T, GATED, SHIFT, 1, 1, 4, 1, 4, 1, 2>(a, st);
+    case 2: return launch_gq4_rows_of<T, GATED, SHIFT, 2, 2, 4, 1, 2, 2, 2>(a, st);
+    default: return launch_gq4_rows_of<T, GATED, SHIFT, 3, 4, 2, 1, 2, 2, 2>(a, st);
     }
 }
 
 // Any number of tokens (arguments are checked where this is called); up: null for a plain product.
 int gq4_launch_rows(const slim_group_q4_layer *layer, const slim_group_q4_layer *up, int shift, const void *X, int64_t x_ld, int32_t m, void *const (&y)[3],
-                    const int64_t (&y_ld)[3], int32_t dtype, hipStream_t st)
+                    const int64_t (&y_ld)[3], int32_t dtype, void *workspace, hipStream_t st)
 {
+    const Gq4Plan plan = gq4_plan_rows(layer->n, layer->k, m, up != nullptr);
     Gq4RowsArgs a{};
+    a.split = Gq4Split{plan.splits > 1 ? static_cast<float *>(workspace) : nullptr, plan.splits, gq4_part_ld(layer->n)};
     a.w[0] = gq4_weights(layer);
     if (up) a.w[1] = gq4_weights(up);
     a.x = X;
@@ -411,14 +441,16 @@ int gq4_launch_rows(const slim_group_q4_layer *layer, const slim_group_q4_layer 
     auto of = [&](auto type, auto gated) {
         typedef decltype(type) T;
         constexpr bool GATED = decltype(gated)::value;
-        return shift == 5 ? launch_gq4_rows_shape<T, GATED, 5>(a, st) : shift == 6 ? launch_gq4_rows_shape<T, GATED, 6>(a, st) : launch_gq4_rows_shape<T, GATED, 7>(a, st);
+        return shift == 5 ? launch_gq4_rows_shape<T, GATED, 5>(a, plan.shape, st) : shift == 6 ? launch_gq4_rows_shape<T, GATED, 6>(a, plan.shape, st) : launch_gq4_rows_shape<T, GATED, 7>(a, plan.shape, st);
     };
     int rc;
     if (dtype == SLIM_F16)
         rc = up ? of(F16{}, std::true_type{}) : of(F16{}, std::false_type{});
     else
         rc = up ? of(BF16{}, std::true_type{}) : of(BF16{}, std::false_type{});
-    return rc != SLIM_OK ? rc : hip_status(hipGetLastError());
+    if (rc != SLIM_OK) return rc;
+    if (plan.splits > 1) return gq4_launch_finish(a.split, m, layer->n, up != nullptr, a.y, a.y_ld, dtype, st);
+    return hip_status(hipGetLastError());
 }
 
 }  // namespace slim

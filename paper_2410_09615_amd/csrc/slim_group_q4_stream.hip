@@ -327,7 +327,7 @@ static void launch_gq4_stream_type(const Gq4StreamArgs &a, int shift, hipStream_
         launch_gq4_stream_shift<T, GATED, 7>(a, st);
 }
 
-// Up to kGq4Few tokens (checked, as all arguments are, where this is called); up: null for a plain product.
+// Few tokens (gq4_streamed; checked, as all arguments are, where this is called); up: null for a plain product.
 int gq4_launch_stream(const slim_group_q4_layer *layer, const slim_group_q4_layer *up, int shift, const void *X, int64_t x_ld, int32_t m, void *const (&y)[3],
                       const int64_t (&y_ld)[3], int32_t dtype, hipStream_t st)
 {

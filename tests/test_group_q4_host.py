@@ -50,7 +50,7 @@ def test_weight_tile_and_values_refuse():
 def test_products_refuse(name):
     f, t = getattr(B.lib(), name), name.endswith("_t")
     ok = dict(layer=_layer(), x=A, x_ld=64 if t else 256, m=4, y=A, y_ld=256 if t else 64, dtype=0)
-    call = lambda **kw: f(*{**ok, **kw}.values(), None)
+    call = lambda **kw: f(*{**ok, **kw}.values(), None, 0, None)
     for kw in ({"layer": None}, {"layer": _layer(codes=None)}, {"layer": _layer(scales=None)}, {"x": None}, {"y": None}):
         assert call(**kw) == B.SLIM_ERR_NULL, kw
     for kw in ({"layer": _layer(n=0)}, {"layer": _layer(k=0)}, {"layer": _layer(group=16)}, {"m": 0}, {"m": -1}, {"x_ld": ok["x_ld"] - 1},
@@ -63,7 +63,7 @@ def test_products_refuse(name):
 def test_gated_refuses():
     f = B.lib().slim_group_q4_gated
     ok = dict(gate=_layer(), up=_layer(zeros=None), x=A, x_ld=256, m=4, h=A, h_ld=64, g=A, g_ld=64, u=A, u_ld=64, dtype=1)
-    call = lambda **kw: f(*{**ok, **kw}.values(), None)
+    call = lambda **kw: f(*{**ok, **kw}.values(), None, 0, None)
     for kw in ({"gate": None}, {"up": None}, {"up": _layer(codes=None)}, {"x": None}, {"h": None}):
         assert call(**kw) == B.SLIM_ERR_NULL, kw
     for kw in ({"up": _layer(n=65)}, {"up": _layer(k=255)}, {"gate": _layer(group=64)}, {"m": 0}, {"x_ld": 255}, {"h_ld": 63}, {"g_ld": 63}, {"u_ld": 0},
@@ -77,7 +77,7 @@ def test_gated_backward_refuses():
     f = B.lib().slim_group_q4_gated_backward
     C, D, E, F, G = (ctypes.c_void_p(0x100000 * i) for i in range(1, 6))
     ok = dict(gate=_layer(), up=_layer(), dh=A, dh_ld=64, g=C, g_ld=64, u=D, u_ld=64, m=4, dg=E, dg_ld=64, du=F, du_ld=64, dx=G, dx_ld=256, dtype=0)
-    call = lambda **kw: f(*{**ok, **kw}.values(), None)
+    call = lambda **kw: f(*{**ok, **kw}.values(), None, 0, None)
     for name in ("gate", "up", "dh", "g", "u", "dg", "du", "dx"):
         assert call(**{name: None}) == B.SLIM_ERR_NULL, name
     for kw in ({"up": _layer(n=65)}, {"up": _layer(group=32)}, {"m": 0}, {"dh_ld": 63}, {"g_ld": 63}, {"u_ld": 63}, {"dg_ld": 63}, {"du_ld": 63}, {"dx_ld": 255},
