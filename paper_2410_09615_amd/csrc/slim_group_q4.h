@@ -10,8 +10,13 @@ namespace slim {
 // lane holds of the four 16 x 16 x 32 products over the block's inputs: its dword j has inputs 32 j + 8 q .. + 7 of row r.  Inputs 2 i and
 // 2 i + 1 of a dword are its nibbles i and i + 4, so that shifting by 4 i and masking leaves the two as 16-bit halves.
 constexpr int kGq4Rows = 16, kGq4Cols = 128, kGq4Block = 1024;
-// Whether weights are streamed (slim_group_q4_stream.hip): up to 48 tokens.
-inline bool gq4_streamed(int n, int m, bool gated) { return m <= 48; }
+// Whether weights are streamed (slim_group_q4_stream.hip): for up to 48 tokens, and on small layers for some more, a workgroup for each 48 of them.  us streamed / in tiles: 64 tokens on
+// 4096 x 4096 12.5 / 18.5, on 5120 x 5120 17.9 / 19.2, on 4096 x 11008 26.2 / 22.9; gated 64 on 4096 x 4096 18.1 / 20.8, on 5120 x 5120 28.8 / 22.7; 144 on 1024 x 4096 8.6 / 16.3, on 4096 x 4096 22.9 / 22.1.
+inline bool gq4_streamed(int n, int k, int m, bool gated)
+{
+    const int64_t weights = (int64_t)n * k * (gated ? 2 : 1);
+    return m <= 48 || (m <= 96 && weights <= 34 << 20) || (m <= 192 && weights <= 8 << 20);
+}
 constexpr int kGq4Sym = 8;                    // the zero point of symmetric weights
 
 inline int gq4_row_blocks(int n) { return (int)(((int64_t)n + kGq4Rows - 1) / kGq4Rows); }
@@ -176,7 +181,7 @@ struct Gq4Shape {
 struct Gq4Plan {
     int shape, splits;
 };
-// The shape and number of splits with the least of rounds x (steps x time + 4 us) and what sums left in memory cost.
+// The shape and number of splits with the least of rounds x (steps x time + 5 us) and what sums left in memory cost.
 template <int N>
 inline Gq4Plan gq4_plan(const Gq4Shape (&shapes)[N], int outs, int m, int steps, bool gated)
 {
@@ -187,9 +192,9 @@ inline Gq4Plan gq4_plan(const Gq4Shape (&shapes)[N], int outs, int m, int steps,
         const Gq4Shape &s = shapes[i];
         const double tiles = (double)(((int64_t)outs * (gated ? 2 : 1) + s.outs - 1) / s.outs) * (double)(((int64_t)m + s.toks - 1) / s.toks);
         for (int splits = 1; splits <= 16 && (splits == 1 || (tiles * splits <= cus * s.per_cu && splits * 8 <= steps)); ++splits) {
-            const double slots = cus * s.per_cu, rounds = __builtin_ceil(tiles * splits / slots), busy = tiles * splits / cus;
+            const double slots = cus * s.per_cu, rounds = __builtin_ceil(tiles * splits / slots), busy = tiles * splits / slots;
             const double step = busy <= 0.5 ? s.few : busy >= 1 ? s.all : s.few + (s.all - s.few) * (busy - 0.5) * 2;
-            double time = rounds * (((steps + splits - 1) / splits) * step + 4);
+            double time = rounds * (((steps + splits - 1) / splits) * step + 5);
             if (splits > 1) time += 4 + (2.0 * (double)gq4_part_bytes(splits, m, outs, gated) + 2.0 * m * outs) / kGq4Reads;
             if ((i == 0 && splits == 1) || time < least) {
                 least = time;

@@ -396,14 +396,11 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
     }
 }
 
-constexpr Gq4Shape kBackShapes[] = {{256, 256, 1, 1.5f, 2.1f}, {256, 128, 1, 1.1f, 1.3f}, {128, 128, 1, 0.75f, 0.9f}, {128, 64, 1, 0.6f, 0.7f}};
+constexpr Gq4Shape kBackShapes[] = {{256, 256, 1, 1.44f, 2.0f}, {256, 128, 1, 1.12f, 1.4f}, {128, 128, 1, 0.65f, 0.78f}, {128, 64, 1, 0.55f, 0.62f}};
 
 static Gq4Plan gq4_plan_back(int n, int k, int m, int terms)
 {
-    Gq4Plan p = gq4_plan(kBackShapes, k, m, n / 64 * terms, false);
-    if (const char *e = getenv("GQ4_T")) p.shape = atoi(e);
-    if (const char *e = getenv("GQ4_Z")) p.splits = atoi(e);
-    return p;
+    return gq4_plan(kBackShapes, k, m, n / 64 * terms, false);
 }
 int64_t gq4_back_workspace(int n, int k, int m, int terms) { return gq4_part_bytes(gq4_plan_back(n, k, m, terms).splits, m, k, false); }
 

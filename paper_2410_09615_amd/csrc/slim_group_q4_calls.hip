@@ -34,7 +34,7 @@ static size_t gq4_need(int32_t n, int32_t k, int32_t m, int32_t call)
     for (const int tokens : {(int)m, 1}) {                           // (one: of a call that goes token by token)
         int64_t b = 0;
         if (call == SLIM_GROUP_Q4_GEMM || call == SLIM_GROUP_Q4_GATED)
-            b = gq4_streamed(n, tokens, call == SLIM_GROUP_Q4_GATED) ? 0 : gq4_rows_workspace(n, k, tokens, call == SLIM_GROUP_Q4_GATED);
+            b = gq4_streamed(n, k, tokens, call == SLIM_GROUP_Q4_GATED) ? 0 : gq4_rows_workspace(n, k, tokens, call == SLIM_GROUP_Q4_GATED);
         else
             b = gq4_back_workspace(n, k, tokens, call == SLIM_GROUP_Q4_GATED_BACKWARD ? 2 : 1);
         most = b > most ? b : most;
@@ -53,7 +53,7 @@ static int gq4_forward(const slim_group_q4_layer *layer, const slim_group_q4_lay
                        const int64_t (&y_ld)[3], int32_t dtype, void *workspace, hipStream_t st)
 {
     if (x_ld < kLongRow || m == 1) {
-        if (gq4_streamed(layer->n, m, up != nullptr)) return gq4_launch_stream(layer, up, shift, X, x_ld, m, y, y_ld, dtype, st);
+        if (gq4_streamed(layer->n, layer->k, m, up != nullptr)) return gq4_launch_stream(layer, up, shift, X, x_ld, m, y, y_ld, dtype, st);
         return gq4_launch_rows(layer, up, shift, X, x_ld, m, y, y_ld, dtype, workspace, st);
     }
     for (int t = 0; t < m; ++t) {

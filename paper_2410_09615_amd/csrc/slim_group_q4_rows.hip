@@ -11,14 +11,11 @@
 
 namespace slim {
 
-constexpr Gq4Shape kRowShapes[] = {{256, 256, 1, 1.24f, 1.94f}, {256, 128, 2, 0.88f, 1.0f}, {256, 64, 1, 0.55f, 0.65f}, {128, 64, 1, 0.38f, 0.5f}};
+constexpr Gq4Shape kRowShapes[] = {{256, 256, 1, 1.2f, 1.9f}, {256, 128, 2, 0.85f, 1.5f}, {256, 64, 1, 0.5f, 0.65f}, {128, 64, 1, 0.3f, 0.38f}};
 
 static Gq4Plan gq4_plan_rows(int n, int k, int m, bool gated)
 {
-    Gq4Plan p = gq4_plan(kRowShapes, n, m, 2 * (k / kGq4Cols), gated);
-    if (const char *e = getenv("GQ4_F")) p.shape = atoi(e);
-    if (const char *e = getenv("GQ4_Z")) p.splits = atoi(e);
-    return p;
+    return gq4_plan(kRowShapes, n, m, 2 * (k / kGq4Cols), gated);
 }
 int64_t gq4_rows_workspace(int n, int k, int m, bool gated) { return gq4_part_bytes(gq4_plan_rows(n, k, m, gated).splits, m, n, gated); }
 
@@ -258,13 +255,11 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
                     } else
                         number(w[n], sc[n & 1], std::integral_constant<int, kk + 1>{}, af[(kk + 1) & 1]);
                     multiply(af[kk & 1], bf[kk & 1]);
-#ifndef NOSGB
 #pragma unroll
                     for (int i = 0; i < AF * BF; ++i) {
                         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                  // a product,
                         __builtin_amdgcn_sched_group_barrier(0x002, BF >= 4 ? 4 : 8, 0);    // and vector instructions that it takes the time of
                     }
-#endif
                     __builtin_amdgcn_sched_barrier(0);
                 });
                 if (++s >= turns) break;

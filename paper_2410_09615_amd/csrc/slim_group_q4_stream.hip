@@ -59,6 +59,8 @@ __global__ __launch_bounds__(THREADS) void gq4_stream_kernel(Gq4StreamArgs a)
     extern __shared__ __align__(16) uint8_t lds[];
     const int S = (int)blockDim.x / kWave, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x & (kWave - 1);
     const int r = lane & 15, q = lane >> 4;
+    const int t0 = (int)blockIdx.y * (16 * TB), toks = min(16 * TB, a.m - t0);          // this workgroup's tokens
+    const uint8_t *const xbase = static_cast<const uint8_t *>(a.x) + (int64_t)t0 * a.x_ld * 2;
     constexpr int PAIRS = GATED ? FR / 2 : FR;
     const int rb0 = (int)blockIdx.x * PAIRS;
     const int whole = a.k / kGq4Cols, share = (whole + S - 1) / S, first = w * share, end = min(first + share, whole);
@@ -83,7 +85,7 @@ __global__ __launch_bounds__(THREADS) void gq4_stream_kernel(Gq4StreamArgs a)
     // the operand needs them, neighbouring lanes would ask for different tokens.  A token's 16 pieces of 16 bytes are in another order in each of 16 rows.
     uint32_t x_at[XI];
 #pragma unroll
-    for (int i = 0; i < XI; ++i) x_at[i] = ((uint32_t)min(4 * i + q, a.m - 1) * (uint32_t)a.x_ld + 8u * (uint32_t)r) * 2u;
+    for (int i = 0; i < XI; ++i) x_at[i] = ((uint32_t)min(4 * i + q, toks - 1) * (uint32_t)a.x_ld + 8u * (uint32_t)r) * 2u;
 
     struct Stage {
         uint4_t c[FR];
@@ -125,7 +127,7 @@ __global__ __launch_bounds__(THREADS) void gq4_stream_kernel(Gq4StreamArgs a)
         wave_lds_order();
     };
     auto load_x = [&](Tokens &x, int b) {
-        const uint8_t *base = static_cast<const uint8_t *>(a.x) + (int64_t)b * (kGq4Cols * 2);
+        const uint8_t *base = xbase + (int64_t)b * (kGq4Cols * 2);
 #pragma unroll
         for (int i = 0; i < XI; ++i) x.v[i] = Piece<T, 8>::load(reinterpret_cast<const E *>(base + x_at[i]));
     };
@@ -222,7 +224,7 @@ __global__ __launch_bounds__(THREADS) void gq4_stream_kernel(Gq4StreamArgs a)
         const int left = a.k - whole * kGq4Cols;
         load_run(run, whole * NG);
         load(st[0], whole);
-        const uint8_t *base = static_cast<const uint8_t *>(a.x) + (int64_t)whole * (kGq4Cols * 2);
+        const uint8_t *base = xbase + (int64_t)whole * (kGq4Cols * 2);
 #pragma unroll
         for (int i = 0; i < XI; ++i)
 #pragma unroll
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(THREADS) void gq4_stream_kernel(Gq4StreamArgs a)
         if (row < a.n) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int tok = 16 * t + 4 * q + e;
+                const int64_t tok = t0 + 16 * t + 4 * q + e;
                 if (tok < a.m) {
                     if constexpr (GATED) {
                         static_cast<E *>(a.y[0])[tok * a.y_ld[0] + row] = (E)(v[e] * gq4_sigma(v[e]) * u[e]);
@@ -271,9 +273,9 @@ __global__ __launch_bounds__(THREADS) void gq4_stream_kernel(Gq4StreamArgs a)
 struct Gq4StreamPlan {
     int blocks, waves, workgroups;
 };
-static Gq4StreamPlan gq4_plan_stream(int rb, int cb, int m, bool gated)
+static Gq4StreamPlan gq4_plan_stream(int rb, int cb, int tb, bool gated)
 {
-    const int cus = device_info().cus, tb = (m + 15) / 16;
+    const int cus = device_info().cus;
     auto cost = [&](int blocks) { return ((rb + blocks * cus - 1) / (blocks * cus)) * (2 * blocks + tb); };
     Gq4StreamPlan p;
     p.blocks = gated || cost(2) <= cost(1) ? 2 : 1;
@@ -292,14 +294,14 @@ static void launch_gq4_stream_of(const Gq4StreamArgs &a, const Gq4StreamPlan &p,
     constexpr int TB = (XI + 3) / 4, D = XI >= 12 ? 2 : 3, THREADS = 512;
     constexpr size_t LDS = Gq4StreamLds<FR, TB>::bytes;
     static_assert(LDS == Gq4StreamLds<FR, 1>::bytes + (TB - 1) * 4096 && (size_t)FR * TB * kWave * 16 <= LDS, "LDS");
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(gq4_stream_kernel<T, GATED, SHIFT, FR, XI, D, THREADS>), dim3((unsigned)p.workgroups), dim3((unsigned)(p.waves * kWave)),
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(gq4_stream_kernel<T, GATED, SHIFT, FR, XI, D, THREADS>), dim3((unsigned)p.workgroups, (unsigned)((a.m + 16 * TB - 1) / (16 * TB))), dim3((unsigned)(p.waves * kWave)),
                        p.waves * LDS, st, a);
 }
 
 template <class T, bool GATED, int SHIFT, int XI>
 static void launch_gq4_stream_tb(const Gq4StreamArgs &a, hipStream_t st)
 {
-    const Gq4StreamPlan p = gq4_plan_stream(a.rb, a.cb, a.m, GATED);
+    const Gq4StreamPlan p = gq4_plan_stream(a.rb, a.cb, XI <= 4 ? 1 : XI / 4, GATED);
     if constexpr (!GATED)
         if (p.blocks == 1) return launch_gq4_stream_of<T, GATED, SHIFT, 1, XI>(a, p, st);
     launch_gq4_stream_of<T, GATED, SHIFT, 2, XI>(a, p, st);
@@ -309,7 +311,8 @@ template <class T, bool GATED, int SHIFT>
 static void launch_gq4_stream_shift(const Gq4StreamArgs &a, hipStream_t st)
 {
     if (a.m <= 4) return launch_gq4_stream_tb<T, GATED, SHIFT, 1>(a, st);
-    switch ((a.m + 15) / 16) {
+    const int chunks = (a.m + 47) / 48;                               // of tokens: up to 48 each, as alike as can be
+    switch (((a.m + chunks - 1) / chunks + 15) / 16) {
     case 1: return launch_gq4_stream_tb<T, GATED, SHIFT, 4>(a, st);
     case 2: return launch_gq4_stream_tb<T, GATED, SHIFT, 8>(a, st);
     default: return launch_gq4_stream_tb<T, GATED, SHIFT, 12>(a, st);

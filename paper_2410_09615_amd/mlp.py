@@ -64,6 +64,34 @@ class DecoderMlp:
         return slim.slim_block_fp8_gemm(self.down, a, a_scales, Y=out, workspace=self._wd), h
 
 
+class GroupMlp:
+    """The same feed-forward part on 4-bit weights with group scales: out = (silu(X Wg^T) * (X Wu^T)) Wd^T, two launches forward for few tokens, and the gradients
+    that the frozen weights pass on (what low-rank terms beside them are trained with).  X is the norm's output, fp16 or bf16.  Calls follow one another on one stream."""
+
+    def __init__(self, gate: slim.SlimGroupQ4Weight, up: slim.SlimGroupQ4Weight, down: slim.SlimGroupQ4Weight, max_tokens: int):
+        if (gate.n, gate.k) != (up.n, up.k) or (down.n, down.k) != (gate.k, gate.n):
+            raise ValueError("gate and up must be [f][k] and down [k][f]")
+        self.gate, self.up, self.down, self.max_tokens = gate, up, down, max_tokens
+        # what a call needs does not grow with its tokens throughout: the most that any number of them does, of the calls in turn
+        room = max(slim.slim_group_q4_workspace(layer.n, layer.k, m, call) for m in range(1, max_tokens + 1)
+                   for layer, call in ((gate, "gated"), (down, "gemm"), (down, "gemm_t"), (gate, "gated_backward")))
+        self._ws = torch.empty(room, dtype=torch.uint8, device=gate.codes.device)
+
+    def forward(self, X: torch.Tensor, keep: bool = False, out: torch.Tensor | None = None):
+        """X [m][k] -> (out [m][k], what backward wants where `keep` is set: H, G, U [m][f])."""
+        if X.shape[0] > self.max_tokens:
+            raise ValueError(f"{X.shape[0]} tokens, made for {self.max_tokens}")
+        saved = slim.slim_group_q4_gated(self.gate, self.up, X, G=True if keep else None, U=True if keep else None, workspace=self._ws)
+        return slim.slim_group_q4_gemm(self.down, saved[0], Y=out, workspace=self._ws), saved if keep else None
+
+    def backward(self, d_out: torch.Tensor, saved):
+        """The gradient of forward's output -> those of X, H, and (in the place of what was kept) G and U."""
+        _, G, U = saved
+        dH = slim.slim_group_q4_gemm_t(self.down, d_out, workspace=self._ws)
+        dX, dG, dU = slim.slim_group_q4_gated_backward(self.gate, self.up, dH, G, U, dG=G, dU=U, workspace=self._ws)
+        return dX, dH, dG, dU
+
+
 def _demo(tokens: int) -> None:
     dev, k, f = torch.device("cuda:0"), 4096, 11008
     g = torch.Generator(device=dev)

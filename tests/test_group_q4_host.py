@@ -141,3 +141,37 @@ def test_oracle_gradients_by_differences():
         e[at] = step
         assert abs(((O.gated(G + e, U) - O.gated(G - e, U)) * dH).sum() / (2 * step) - dG[at]) < 1e-7
         assert abs(((O.gated(G, U + e) - O.gated(G, U - e)) * dH).sum() / (2 * step) - dU[at]) < 1e-7
+
+
+def test_workspaces():
+    """Few tokens forward need none; where tiles are shared a call without room is refused before anything is launched."""
+    for n, k in ((1, 1), (4096, 4096), (28672, 8192)):
+        for call in ("gemm", "gated"):
+            assert all(B.slim_group_q4_workspace(n, k, m, call) == 0 for m in (1, 2, 16, 17, 48))
+    need = B.slim_group_q4_workspace(4096, 4096, 200, "gemm_t")
+    assert need > 0 and need % (200 * 4096 * 4) == 0
+    f = B.lib().slim_group_q4_gemm_t
+    big = _layer(n=4096, k=4096)
+    assert f(big, A, 4096, 200, A, 4096, 0, None, 0, None) == B.SLIM_ERR_WORKSPACE
+    assert f(big, A, 4096, 200, A, 4096, 0, A, need - 1, None) == B.SLIM_ERR_WORKSPACE
+    assert f(big, A, 4096, 200, A, 4096, 0, HALF, need, None) == B.SLIM_ERR_ALIGN
+    out = ctypes.c_size_t()
+    assert B.lib().slim_group_q4_workspace(5, 5, 1, 0, None) == B.SLIM_ERR_NULL
+    for bad in ((0, 5, 1, 0), (5, 0, 1, 0), (5, 5, 0, 0), (5, 5, 1, 4), (5, 5, 1, -1)):
+        assert B.lib().slim_group_q4_workspace(*bad, out) == B.SLIM_ERR_SHAPE, bad
+
+
+def test_another_device_is_made_current_for_the_call(monkeypatch):
+    """What the binding does where the tensors' device is not the current one (status 2), and where a layer's data has moved (1) or room is wanted."""
+    seen = []
+    monkeypatch.setattr(B.torch.cuda, "device", lambda d: __import__("contextlib").nullcontext(seen.append(d)))
+    monkeypatch.setattr(B, "alloc_group_q4_workspace", lambda layer, m, call: ("room", m, call))
+    calls = []
+
+    def call(again, ws):
+        calls.append((again, ws))
+        return {1: 2, 2: B.SLIM_ERR_WORKSPACE, 3: 0}[len(calls)]
+    B._q4_call("slim_group_q4_gemm_t", None, 5, 7, None, 1, call)
+    assert seen == [5] and calls == [(True, None), (False, None), (False, ("room", 7, "gemm_t"))]
+    with pytest.raises(B.SlimError):
+        B._q4_call("slim_group_q4_gemm", None, 0, 1, "small", B.SLIM_ERR_WORKSPACE, call)
