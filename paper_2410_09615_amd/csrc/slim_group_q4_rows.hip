@@ -46,8 +46,8 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
     constexpr int AF = 2, THREADS = WR * WT * kWave, BO = 32 * AF * WR, BT = 32 * BF * WT, UNROLL = RW;
     constexpr int NG = kGq4Cols >> SHIFT, PER = 4 / NG;                       // groups per block, products of a step per group
     typedef Gq4RowsLds<KG, BO, BT> Lds;
-    constexpr int STAGE = Lds::stage, TABLE = Lds::table, XTASKS = BT * 8 / THREADS, ITEMS = BO * 8 / THREADS;
-    static_assert(XTASKS * THREADS == BT * 8 && ITEMS * THREADS == BO * 8 && RW % RX == 0 && RW % 2 == 0, "tile");
+    constexpr int STAGE = Lds::stage, TABLE = Lds::table, XTASKS = BT * 8 / THREADS, ITEMS = BO * 2 / THREADS;
+    static_assert(XTASKS * THREADS == BT * 8 && ITEMS * THREADS == BO * 2 && RW % RX == 0 && RW % 2 == 0, "tile");
     extern __shared__ __align__(16) uint8_t lds[];
     const Gq4Masks masks;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x & (kWave - 1);
@@ -101,27 +101,38 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
         *reinterpret_cast<uint4_t *>(to + xl_at[i]) = there ? __builtin_bit_cast(uint4_t, v.x[i]) : uint4_t{0, 0, 0, 0};
     };
     // ---- scales and zero points: windows of 8 groups of the tile's rows in LDS, two, filled one ahead ----
-    // Where each lane fetches the scale of its own row, neighbouring lanes ask the memory pipeline for different lines, which takes four times as long as when they share one: so
-    // eight lanes fetch the eight groups of a row.
+    // Where each lane fetches the scale of its own row every step, neighbouring lanes ask the memory pipeline for different lines, which takes four times as long as when they share one.
+    // A thread fetches four groups of a row.  Near a row's end they are fetched from four before the end and moved down to their places.
     struct Window {
-        half_t s[ITEMS];
+        uint2_t s[ITEMS];
         uint32_t z[ITEMS];
     };
     Window ahead;
     auto load_window = [&](int w) {
-        const int wave_row = gw * 8;                                          // (a wavefront's items of one i are of one layer)
+        const int wave_row = gw * 32;                                         // (a wavefront's items of one i are of one layer)
         int own_tid = tid;                                                    // (made anew here each time: kept over the loop, what follows from it takes too many registers)
         asm volatile("" : "+v"(own_tid));
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int item = own_tid + i * THREADS, row = item / 8, g = item % 8;
-            const Gq4Weights &l = GATED && ((i * (THREADS / 8) + wave_row) & 32) ? a.w[1] : a.w[0];
+            const int item = own_tid + i * THREADS, row = item / 2, g = 8 * w + 4 * (item % 2), from = max(min(g, a.kg - 4), 0);
+            const Gq4Weights &l = GATED && ((i * (THREADS / 2) + wave_row) & 32) ? a.w[1] : a.w[0];
             const int local = GATED ? (row >> 6) * 32 + (row & 31) : row;
             const uint8_t *scales = reinterpret_cast<const uint8_t *>(l.scales + (int64_t)o0 * a.kg);
             const uint8_t *zeros = l.zeros ? l.zeros + (int64_t)o0 * a.kg : scales;          // (symmetric: what is read of the scales instead is not used)
-            const uint32_t place = (uint32_t)min(local, a.n - 1 - o0) * (uint32_t)a.kg + (uint32_t)min(8 * w + g, a.kg - 1);
-            ahead.s[i] = *reinterpret_cast<const half_t *>(scales + place * 2u);
-            ahead.z[i] = *(zeros + place);
+            const uint32_t place = (uint32_t)min(local, a.n - 1 - o0) * (uint32_t)a.kg + (uint32_t)from;
+            if (a.kg >= 4) {
+                ahead.s[i] = reinterpret_cast<const Gq4Any<uint2_t> *>(scales + place * 2u)->v;
+                ahead.z[i] = reinterpret_cast<const Gq4Any<uint32_t> *>(zeros + place)->v;
+            } else {
+                ahead.s[i] = uint2_t{0, 0};
+                ahead.z[i] = 0;
+#pragma unroll
+                for (int e = 0; e < 3; ++e) {
+                    const uint32_t at = place + (uint32_t)min(e, a.kg - 1);
+                    ahead.s[i][e / 2] |= (uint32_t) * reinterpret_cast<const uint16_t *>(scales + at * 2u) << (16 * (e & 1));
+                    ahead.z[i] |= (uint32_t)zeros[at] << (8 * e);
+                }
+            }
         }
     };
     auto put_window = [&](int w) {
@@ -130,10 +141,12 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
         asm volatile("" : "+v"(own_tid));
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int item = own_tid + i * THREADS, row = item / 8, g = item % 8;
+            const int item = own_tid + i * THREADS, row = item / 2, g = 8 * w + 4 * (item % 2), down = g - max(min(g, a.kg - 4), 0);
             const bool points = (GATED && (row & 32) ? a.w[1].zeros : a.w[0].zeros) != nullptr;
-            *reinterpret_cast<half_t *>(t + row * 24 + g * 2) = ahead.s[i];
-            t[row * 24 + 16 + g] = points ? (uint8_t)ahead.z[i] : (uint8_t)kGq4Sym;
+            // (groups that are not there, whose places get anything, may be all four)
+            const uint64_t s = (uint64_t)ahead.s[i][1] << 32 | ahead.s[i][0];
+            *reinterpret_cast<uint64_t *>(t + row * 24 + (item % 2) * 8) = s >> (16 * (down & 3));
+            *reinterpret_cast<uint32_t *>(t + row * 24 + 16 + (item % 2) * 4) = points ? ahead.z[i] >> (8 * (down & 3)) : 0x01010101u * kGq4Sym;
         }
     };
     auto window_of = [&](int step) { return step >> (SHIFT - 3); };            // a block has NG groups, a window 8: two steps a block
