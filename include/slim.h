@@ -638,6 +638,13 @@ typedef enum { SLIM_GROUP_Q4_GEMM = 0, SLIM_GROUP_Q4_GATED = 1, SLIM_GROUP_Q4_GE
 int slim_group_q4_workspace(int32_t n, int32_t k, int32_t m, int32_t call, size_t *bytes);
 
 /*
+ * slim_group_q4_plan -- what a call would launch on the current device, for inspection and tests (no launch): out int32 [4] (HOST) = kernel (0: weights streamed, 1: tiles, weights in
+ * registers, 2: tiles of a gradient), outputs and tokens of a workgroup's tile (streamed: rows of weights, of a gated block both layers'), and the workgroups that share a tile (streamed: the
+ * wavefronts that share the inputs).  Errors: NULL, SHAPE.
+ */
+int slim_group_q4_plan(int32_t n, int32_t k, int32_t m, int32_t call, int32_t *out);
+
+/*
  * slim_group_q4_gemm   -- Y = X W^T:  X [m][k], Y [m][n] of `dtype` (SLIM_F16, SLIM_BF16), any m >= 1.
  * slim_group_q4_gemm_t -- dX = dY W:  the gradient of X through frozen weights; dY [m][n], dX [m][k].
  * Sums in binary32, one rounding of each result.

@@ -56,7 +56,7 @@ EXPORTS = ["slim_status_string", "slim_rank_pad", "slim_packed_sizes", "slim_pac
            "slim_block_fp8_tile", "slim_block_fp8_untile", "slim_block_fp8_gemm_workspace", "slim_block_fp8_gemm",
            "slim_block_fp8_gemm_plan",
            "slim_group_q4_sizes", "slim_group_q4_weight", "slim_group_q4_tile", "slim_group_q4_untile", "slim_group_q4_values", "slim_group_q4_gemm",
-           "slim_group_q4_gemm_t", "slim_group_q4_gated", "slim_group_q4_gated_backward", "slim_group_q4_workspace"]
+           "slim_group_q4_gemm_t", "slim_group_q4_gated", "slim_group_q4_gated_backward", "slim_group_q4_workspace", "slim_group_q4_plan"]
 
 
 def lib():
@@ -117,6 +117,7 @@ def lib():
         L.slim_group_q4_tile.argtypes = [vp, i64, i32, i32, vp, vp]
         L.slim_group_q4_untile.argtypes = [vp, i32, i32, vp, i64, vp]
         L.slim_group_q4_values.argtypes = [pq4, vp, i64, i32, vp]
+        L.slim_group_q4_plan.argtypes = [i32, i32, i32, i32, pi32]
         L.slim_group_q4_workspace.argtypes = [i32, i32, i32, i32, psz]
         L.slim_group_q4_gemm.argtypes = L.slim_group_q4_gemm_t.argtypes = [pq4, vp, i64, i32, vp, i64, i32, vp, sz, vp]
         L.slim_group_q4_gated.argtypes = [pq4, pq4, vp, i64, i32, vp, i64, vp, i64, vp, i64, i32, vp, sz, vp]
@@ -944,6 +945,13 @@ def slim_group_q4_workspace(n: int, k: int, m: int, call: str = "gemm") -> int:
     out = ctypes.c_size_t()
     _check("slim_group_q4_workspace", lib().slim_group_q4_workspace(n, k, m, Q4_CALLS[call], out))
     return out.value
+
+
+def slim_group_q4_plan(n: int, k: int, m: int, call: str = "gemm") -> dict:
+    """What a call would launch (host logic; no launch): kernel "stream", "tile" or "back", outputs and tokens of a workgroup's tile, and what shares it: workgroups, or ("stream") wavefronts."""
+    out = (ctypes.c_int32 * 4)()
+    _check("slim_group_q4_plan", lib().slim_group_q4_plan(n, k, m, Q4_CALLS[call], out))
+    return {"kernel": ("stream", "tile", "back")[out[0]], "outputs": out[1], "tokens": out[2], "shared": out[3]}
 
 
 def alloc_group_q4_workspace(layer: SlimGroupQ4Weight, m: int, call: str = "gemm") -> torch.Tensor:

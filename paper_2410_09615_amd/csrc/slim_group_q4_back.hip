@@ -402,6 +402,13 @@ static Gq4Plan gq4_plan_back(int n, int k, int m, int terms)
 {
     return gq4_plan(kBackShapes, k, m, n / 64 * terms, false);
 }
+void gq4_back_plan(int n, int k, int m, int terms, int32_t *out)
+{
+    const Gq4Plan p = gq4_plan_back(n, k, m, terms);
+    out[1] = kBackShapes[p.shape].outs;
+    out[2] = kBackShapes[p.shape].toks;
+    out[3] = p.splits;
+}
 int64_t gq4_back_workspace(int n, int k, int m, int terms) { return gq4_part_bytes(gq4_plan_back(n, k, m, terms).splits, m, k, false); }
 
 template <class T, int SHIFT, int SHAPE, int KG, int P, int WR, int WT, int AF, int BF>

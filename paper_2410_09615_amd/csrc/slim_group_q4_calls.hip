@@ -13,6 +13,9 @@ int gq4_launch_rows(const slim_group_q4_layer *layer, const slim_group_q4_layer 
                     const int64_t (&y_ld)[3], int32_t dtype, void *workspace, hipStream_t st);
 int gq4_launch_back(const slim_group_q4_layer *one, const slim_group_q4_layer *second, int shift, const void *dY, int64_t ld, const void *dY2, int64_t ld2, int32_t m, void *dX,
                     int64_t dx_ld, int32_t dtype, void *workspace, hipStream_t st);
+void gq4_stream_plan(int n, int k, int m, bool gated, int32_t *out);
+void gq4_rows_plan(int n, int k, int m, bool gated, int32_t *out);
+void gq4_back_plan(int n, int k, int m, int terms, int32_t *out);
 int64_t gq4_rows_workspace(int n, int k, int m, bool gated);
 int64_t gq4_back_workspace(int n, int k, int m, int terms);
 
@@ -86,6 +89,27 @@ extern "C" int slim_group_q4_workspace(int32_t n, int32_t k, int32_t m, int32_t 
     if (!bytes) return SLIM_ERR_NULL;
     if (slim_group_q4_sizes(n, k, 128, nullptr, nullptr, nullptr) != SLIM_OK || m < 1 || call < SLIM_GROUP_Q4_GEMM || call > SLIM_GROUP_Q4_GATED_BACKWARD) return SLIM_ERR_SHAPE;
     *bytes = gq4_need(n, k, m, call);
+    return SLIM_OK;
+}
+
+// What a call would launch (no launch, no device access but for its number of compute units).
+extern "C" int slim_group_q4_plan(int32_t n, int32_t k, int32_t m, int32_t call, int32_t *out)
+{
+    size_t need;
+    if (!out) return SLIM_ERR_NULL;
+    const int status = slim_group_q4_workspace(n, k, m, call, &need);
+    if (status != SLIM_OK) return status;
+    const bool gated = call == SLIM_GROUP_Q4_GATED;
+    if (gated || call == SLIM_GROUP_Q4_GEMM) {
+        out[0] = gq4_streamed(n, k, m, gated) ? 0 : 1;
+        if (out[0] == 0)
+            gq4_stream_plan(n, k, m, gated, out);
+        else
+            gq4_rows_plan(n, k, m, gated, out);
+    } else {
+        out[0] = 2;
+        gq4_back_plan(n, k, m, call == SLIM_GROUP_Q4_GATED_BACKWARD ? 2 : 1, out);
+    }
     return SLIM_OK;
 }
 

@@ -11,11 +11,18 @@
 
 namespace slim {
 
-constexpr Gq4Shape kRowShapes[] = {{256, 256, 1, 1.2f, 1.9f}, {256, 128, 2, 0.85f, 1.5f}, {256, 64, 1, 0.5f, 0.65f}, {128, 64, 1, 0.3f, 0.38f}};
+constexpr Gq4Shape kRowShapes[] = {{256, 128, 2, 0.85f, 1.9f}, {256, 64, 1, 0.5f, 0.65f}, {128, 64, 1, 0.3f, 0.38f}};
 
 static Gq4Plan gq4_plan_rows(int n, int k, int m, bool gated)
 {
     return gq4_plan(kRowShapes, n, m, 2 * (k / kGq4Cols), gated);
+}
+void gq4_rows_plan(int n, int k, int m, bool gated, int32_t *out)
+{
+    const Gq4Plan p = gq4_plan_rows(n, k, m, gated);
+    out[1] = kRowShapes[p.shape].outs;
+    out[2] = kRowShapes[p.shape].toks;
+    out[3] = p.splits;
 }
 int64_t gq4_rows_workspace(int n, int k, int m, bool gated) { return gq4_part_bytes(gq4_plan_rows(n, k, m, gated).splits, m, n, gated); }
 
@@ -36,14 +43,14 @@ struct Gq4RowsLds {
     static constexpr int stage = BT * 128, table = BO * 24, bytes = KG * 2 * (stage + table);
 };
 
-// A step is half a block of 128 inputs: 16 of each 32, so that a lane's 16 bytes of codes are all it needs of a block of rows.  KG groups of WR x WT wavefronts share the steps, a run
+// A step is half a block of 128 inputs: 16 of each 32, so that a lane's 16 bytes of codes are all it needs of a block of rows.  KG groups of WR wavefronts share the steps, a run
 // of them each.  Weights of RW steps and tokens of RX are in registers or on their way there; tokens go into one buffer of LDS while the other is multiplied from.
-template <class T, bool GATED, int SHIFT, int KG, int WR, int WT, int BF, int RX, int RW>
-__global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsArgs a)
+template <class T, bool GATED, int SHIFT, int KG, int WR, int BF, int RX, int RW>
+__global__ __launch_bounds__(KG *WR *kWave, 2) void gq4_rows_kernel(Gq4RowsArgs a)
 {
     typedef typename T::type E;
     typedef typename Gq4Vec<T>::v8 vec8;
-    constexpr int AF = 2, THREADS = WR * WT * kWave, BO = 32 * AF * WR, BT = 32 * BF * WT, UNROLL = RW;
+    constexpr int AF = 2, THREADS = WR * kWave, BO = 32 * AF * WR, BT = 32 * BF, UNROLL = RW;
     constexpr int NG = kGq4Cols >> SHIFT, PER = 4 / NG;                       // groups per block, products of a step per group
     typedef Gq4RowsLds<KG, BO, BT> Lds;
     constexpr int STAGE = Lds::stage, TABLE = Lds::table, XTASKS = BT * 8 / THREADS, ITEMS = BO * 2 / THREADS;
@@ -51,8 +58,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
     extern __shared__ __align__(16) uint8_t lds[];
     const Gq4Masks masks;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x & (kWave - 1);
-    const int group = KG > 1 ? wave / (WR * WT) : 0, gw = KG > 1 ? wave % (WR * WT) : wave, tid = gw * kWave + lane;
-    const int wr = gw % WR, wt = gw / WR;
+    const int group = KG > 1 ? wave / WR : 0, wr = KG > 1 ? wave % WR : wave, tid = wr * kWave + lane;
     const int gx = a.tiles_o * a.tiles_t;
     const int qx = gx % kDies == 0 ? ((int)blockIdx.x % kDies) * (gx / kDies) + (int)blockIdx.x / kDies : (int)blockIdx.x;
     const int tile = blocked_tile(qx, a.tiles_o, a.tiles_t);
@@ -109,7 +115,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
     };
     Window ahead;
     auto load_window = [&](int w) {
-        const int wave_row = gw * 32;                                         // (a wavefront's items of one i are of one layer)
+        const int wave_row = wr * 32;                                         // (a wavefront's items of one i are of one layer)
         int own_tid = tid;                                                    // (made anew here each time: kept over the loop, what follows from it takes too many registers)
         asm volatile("" : "+v"(own_tid));
 #pragma unroll
@@ -160,7 +166,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
             for (int e = 0; e < 16; ++e) acc[i][t][e] = 0.f;
 
     const uint32_t fr = (uint32_t)lane & 31u, turned = ((uint32_t)lane >> 5 ^ gq4_turn(fr)) * 16u;
-    const uint32_t xl_from = (uint32_t)(wt * BF * 32) * 128u + fr * 128u, s_from = ((uint32_t)(wr * AF * 32) + fr) * 24u;
+    const uint32_t xl_from = fr * 128u, s_from = ((uint32_t)(wr * AF * 32) + fr) * 24u;
     auto read = [&](const uint8_t *from, int kk, vec8 (&bf)[BF]) {
 #pragma unroll
         for (int t = 0; t < BF; ++t) bf[t] = *reinterpret_cast<const vec8 *>(from + xl_from + (turned ^ (uint32_t)kk * 32u) + t * 4096);
@@ -341,7 +347,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
             for (int i = 0; i < AF; ++i)
 #pragma unroll
                 for (int t = 0; t < BF; ++t) {
-                    const int tok = t0 + (wt * BF + t) * 32 + (lane & 31), o = o0 + (GATED ? (wr * AF + i) / 2 : wr * AF + i) * 32 + 4 * (lane >> 5);
+                    const int tok = t0 + t * 32 + (lane & 31), o = o0 + (GATED ? (wr * AF + i) / 2 : wr * AF + i) * 32 + 4 * (lane >> 5);
                     float *const row = a.split.part + (((int64_t)blockIdx.y * (GATED ? 2 : 1) + (GATED ? i & 1 : 0)) * a.m + tok) * a.split.ld + o;
                     if (tok < a.m)
 #pragma unroll
@@ -367,7 +373,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
                     vec4 v;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[e] = (E)value(i, t, 4 * g + e);
-                    const int tok = (wt * BF + t) * 32 + (lane & 31), c = ((GATED ? (wr * AF + i) / 2 : wr * AF + i) * 32 + 8 * g) / 8;
+                    const int tok = t * 32 + (lane & 31), c = ((GATED ? (wr * AF + i) / 2 : wr * AF + i) * 32 + 8 * g) / 8;
                     *reinterpret_cast<vec4 *>(lds + (tok * PER_ROW + (c ^ (tok & TURN))) * 16 + (lane >> 5) * 8) = v;
                 }
         __syncthreads();
@@ -398,10 +404,10 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_rows_kernel(Gq4RowsA
         leave(a.y[0], a.y_ld[0], [&](int i, int t, int e) { return acc[i][t][e]; });
 }
 
-template <class T, bool GATED, int SHIFT, int SHAPE, int KG, int WR, int WT, int BF, int RX, int RW>
+template <class T, bool GATED, int SHIFT, int SHAPE, int KG, int WR, int BF, int RX, int RW>
 static int launch_gq4_rows_of(Gq4RowsArgs a, hipStream_t st)
 {
-    constexpr int THREADS = KG * WR * WT * kWave, BO = 64 * WR, BT = 32 * BF * WT;
+    constexpr int THREADS = KG * WR * kWave, BO = 64 * WR, BT = 32 * BF;
     constexpr size_t OUT = (size_t)BO * BT * 2 / (GATED ? 2 : 1), SUMS = KG > 1 ? (size_t)BO * BT * 4 : 0, RING = Gq4RowsLds<KG, BO, BT>::bytes;
     constexpr size_t LDS = RING > OUT ? (RING > SUMS ? RING : SUMS) : OUT > SUMS ? OUT : SUMS;
     static_assert(LDS * kRowShapes[SHAPE].per_cu <= 160 * 1024 && kRowShapes[SHAPE].outs == BO && kRowShapes[SHAPE].toks == BT, "the table's tile");
@@ -410,7 +416,7 @@ static int launch_gq4_rows_of(Gq4RowsArgs a, hipStream_t st)
     a.tiles_t = (int)(((int64_t)a.m + BT - 1) / BT);
     const int64_t tiles = (int64_t)a.tiles_o * a.tiles_t;
     if (tiles * THREADS > UINT32_MAX) return SLIM_ERR_SHAPE;
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(gq4_rows_kernel<T, GATED, SHIFT, KG, WR, WT, BF, RX, RW>), dim3((unsigned)tiles, (unsigned)a.split.splits), dim3(THREADS), LDS, st, a);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(gq4_rows_kernel<T, GATED, SHIFT, KG, WR, BF, RX, RW>), dim3((unsigned)tiles, (unsigned)a.split.splits), dim3(THREADS), LDS, st, a);
     return SLIM_OK;
 }
 
@@ -418,10 +424,9 @@ template <class T, bool GATED, int SHIFT>
 static int launch_gq4_rows_shape(const Gq4RowsArgs &a, int shape, hipStream_t st)
 {
     switch (shape) {
-    case 0: return launch_gq4_rows_of<T, GATED, SHIFT, 0, 1, 4, 2, 4, 1, 2>(a, st);
-    case 1: return launch_gq4_rows_of<T, GATED, SHIFT, 1, 1, 4, 1, 4, 1, 2>(a, st);
-    case 2: return launch_gq4_rows_of<T, GATED, SHIFT, 2, 2, 4, 1, 2, 2, 2>(a, st);
-    default: return launch_gq4_rows_of<T, GATED, SHIFT, 3, 4, 2, 1, 2, 2, 2>(a, st);
+    case 0: return launch_gq4_rows_of<T, GATED, SHIFT, 0, 1, 4, 4, 1, 2>(a, st);
+    case 1: return launch_gq4_rows_of<T, GATED, SHIFT, 1, 2, 4, 2, 2, 2>(a, st);
+    default: return launch_gq4_rows_of<T, GATED, SHIFT, 2, 4, 2, 2, 2, 2>(a, st);
     }
 }
 

@@ -288,6 +288,18 @@ static Gq4StreamPlan gq4_plan_stream(int rb, int cb, int tb, bool gated)
     return p;
 }
 
+// of a call's tokens: workgroups for so many each, up to 48 and as alike as can be
+static int gq4_stream_chunks(int m) { return (m + 47) / 48; }
+static int gq4_stream_tiles(int m) { return ((m + gq4_stream_chunks(m) - 1) / gq4_stream_chunks(m) + 15) / 16; }
+
+void gq4_stream_plan(int n, int k, int m, bool gated, int32_t *out)
+{
+    const Gq4StreamPlan p = gq4_plan_stream(gq4_row_blocks(n), gq4_col_blocks(k), gq4_stream_tiles(m), gated);
+    out[1] = p.blocks * kGq4Rows;
+    out[2] = m <= 4 ? 4 : 16 * gq4_stream_tiles(m);
+    out[3] = p.waves;
+}
+
 template <class T, bool GATED, int SHIFT, int FR, int XI>
 static void launch_gq4_stream_of(const Gq4StreamArgs &a, const Gq4StreamPlan &p, hipStream_t st)
 {
@@ -311,8 +323,7 @@ template <class T, bool GATED, int SHIFT>
 static void launch_gq4_stream_shift(const Gq4StreamArgs &a, hipStream_t st)
 {
     if (a.m <= 4) return launch_gq4_stream_tb<T, GATED, SHIFT, 1>(a, st);
-    const int chunks = (a.m + 47) / 48;                               // of tokens: up to 48 each, as alike as can be
-    switch (((a.m + chunks - 1) / chunks + 15) / 16) {
+    switch (gq4_stream_tiles(a.m)) {
     case 1: return launch_gq4_stream_tb<T, GATED, SHIFT, 4>(a, st);
     case 2: return launch_gq4_stream_tb<T, GATED, SHIFT, 8>(a, st);
     default: return launch_gq4_stream_tb<T, GATED, SHIFT, 12>(a, st);
