@@ -38,7 +38,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
     constexpr int THREADS = WR * WT * kWave, BO = 32 * AF * WR, BT = 32 * BF * WT;
     typedef Gq4BackLds<KG, BO, BT> Lds;
     constexpr int STAGE = Lds::stage, TABLE = Lds::table, XTASKS = BT * 8 / THREADS, WTASKS = BO * 2 / THREADS;
-    static_assert(XTASKS * THREADS == BT * 8 && WTASKS * THREADS == BO * 2 && BO % 128 == 0, "tile");
+    static_assert(XTASKS * THREADS == BT * 8 && WTASKS * THREADS == BO * 2 && BO % 128 == 0 && AF % 2 == 0, "tile");
     extern __shared__ __align__(16) uint8_t lds[];
     const Gq4Masks masks;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = (int)threadIdx.x & (kWave - 1);
@@ -65,9 +65,10 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
     const uint32_t w_at = (lq * 16u + 4u * lp) * 16u + lj * 4u;
 #pragma unroll
     for (int i = 0; i < WTASKS; ++i) {
-        // input e of the lane's eight: 128 e bytes on, its 16-byte pieces in another order (gq4_turn of an input's row is e ^ q)
+        // Input e of the lane's eight: 128 e bytes on, its 16-byte pieces in another order: e ^ q ^ 4 (j % 2), so that a store of 64 lanes, whose inputs are all 128 bytes or more apart,
+        // finds all banks (with gq4_turn's e ^ q half of them: 37 % of LDS's cycles were waits).
         const uint32_t b = (uint32_t)(gw + i * (WR * WT)), col = (b >> 2) * 128u + 32u * lj + 8u * lq;
-        wl_at[i] = col * 128u + (((b & 3u) * 2u + (lp >> 1)) ^ lq) * 16u + (lp & 1u) * 8u;
+        wl_at[i] = col * 128u + (((b & 3u) * 2u + (lp >> 1)) ^ lq ^ (lj & 1u) * 4u) * 16u + (lp & 1u) * 8u;
     }
     auto weights = [&](int term) {
 #pragma unroll
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
     const uint32_t wl_from = (uint32_t)(wr * AF * 32) * 128u + fr * 128u, xl_from = (uint32_t)(BO + wt * BF * 32) * 128u + fr * 128u;
     auto read = [&](const uint8_t *from, int kk, vec8 (&af)[AF], vec8 (&bf)[BF]) {
 #pragma unroll
-        for (int i = 0; i < AF; ++i) af[i] = *reinterpret_cast<const vec8 *>(from + wl_from + (turned ^ (uint32_t)kk * 32u) + i * 4096);
+        for (int i = 0; i < AF; ++i) af[i] = *reinterpret_cast<const vec8 *>(from + wl_from + (turned ^ (uint32_t)(kk * 32 ^ (i & 1) * 64)) + i * 4096);
 #pragma unroll
         for (int t = 0; t < BF; ++t) bf[t] = *reinterpret_cast<const vec8 *>(from + xl_from + (turned ^ (uint32_t)kk * 32u) + t * 4096);
     };
