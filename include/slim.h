@@ -647,7 +647,9 @@ int slim_group_q4_plan(int32_t n, int32_t k, int32_t m, int32_t call, int32_t *o
 /*
  * slim_group_q4_gemm   -- Y = X W^T:  X [m][k], Y [m][n] of `dtype` (SLIM_F16, SLIM_BF16), any m >= 1.
  * slim_group_q4_gemm_t -- dX = dY W:  the gradient of X through frozen weights; dY [m][n], dX [m][k].
- * Sums in binary32, one rounding of each result.
+ * Sums in binary32, one rounding of each result.  Up to 48 tokens forward (on small layers up to 192: slim_group_q4_plan) weights are multiplied as whole numbers c - z and scales applied
+ * to the sums; elsewhere a weight is (c - z) s rounded to `dtype` first, at most half a step of it: 1.9e-4 (fp16) or 1.5e-3 (bf16) of a result in the 2-norm beside the 2.1e-4 or
+ * 1.7e-3 of its own rounding.  A token's result can so differ between calls of few and of many tokens.
  * X, Y (dY, dX) do not overlap.  Errors: NULL, SHAPE, ALIGN, WORKSPACE, HIP.
  */
 int slim_group_q4_gemm(const slim_group_q4_layer *layer, const void *X, int64_t x_ld, int32_t m, void *Y, int64_t y_ld, int32_t dtype, void *workspace,
@@ -659,7 +661,7 @@ int slim_group_q4_gemm_t(const slim_group_q4_layer *layer, const void *dY, int64
  * slim_group_q4_gated -- the first half of a gated feed-forward block in one kernel:
  *   G = X Wg^T,  U = X Wu^T,  H = silu(G) * U  (silu(g) = g / (1 + exp(-g))),
  * gate and up of one n, k and group (each with zero points or without); G and U in binary32 inside.  H [m][n]; G and U, where they are given, receive
- * them rounded: what the backward call wants.
+ * them rounded: what the backward call wants.  X, H, G and U do not overlap.
  * slim_group_q4_gated_backward -- gradients through the block, its weights frozen:
  *   dU = dH silu(G),  dG = dH U sigma(G) (1 + G (1 - sigma(G))),  dX = dG Wg + dU Wu,
  * all of `dtype`; dG and dU [m][n] (what a low-rank term beside the layers needs) are rounded once, and dX is the product of the rounded ones.

@@ -30,6 +30,9 @@ struct Gq4BackLds {
 // A workgroup has a tile of BT tokens x BO inputs and goes over the layers' rows 64 at a time.  KG groups of WR x WT wavefronts take turns at those pieces, each with two buffers of its own
 // in LDS.  While a piece is multiplied from one, the next one goes from registers into the other, and the one P further is asked for from memory into the registers that this frees: beside
 // each quarter of a piece's products (16 rows) stands a part of that work.  Rows that do not fill a piece are left for last and taken without that overlap.
+// Many tokens (256 x 256): 4096 through 8192 x 8192 in fp16 500 us, 1.10 PFLOP/s; through 2 x 11008 x 4096 in bf16 732 to 763 us with the activation's gradient (74), matrix pipes 58 % busy at 1.74 GHz.  LDS
+// carries 256 KiB for a piece's 256 products, about as long as they take, and the two overlap in part: without products 336 us of the 500, without stores to LDS 290.  (Half of the wavefronts at
+// products while the others store, in turn: 599 us.)  Smaller tiles are bound by the chain between two barriers, read, convert, store: 1.3 us a turn on 128 x 128 whose products take 0.2.
 template <class T, int SHIFT, int KG, int P, int WR, int WT, int AF, int BF>
 __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackArgs a)
 {
@@ -66,7 +69,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
 #pragma unroll
     for (int i = 0; i < WTASKS; ++i) {
         // Input e of the lane's eight: 128 e bytes on, its 16-byte pieces in another order: e ^ q ^ 4 (j % 2), so that a store of 64 lanes, whose inputs are all 128 bytes or more apart,
-        // finds all banks (with gq4_turn's e ^ q half of them: 37 % of LDS's cycles were waits).
+        // finds all banks (with gq4_turn's e ^ q half of them: 37 % of LDS's cycles were waits on 256 x 256, now 17 %).
         const uint32_t b = (uint32_t)(gw + i * (WR * WT)), col = (b >> 2) * 128u + 32u * lj + 8u * lq;
         wl_at[i] = col * 128u + (((b & 3u) * 2u + (lp >> 1)) ^ lq ^ (lj & 1u) * 4u) * 16u + (lp & 1u) * 8u;
     }
@@ -397,6 +400,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
     }
 }
 
+// Inputs and tokens of a tile, workgroups per compute unit, us per step of 64 rows.
 constexpr Gq4Shape kBackShapes[] = {{256, 256, 1, 1.44f, 2.0f}, {256, 128, 1, 1.12f, 1.4f}, {128, 128, 1, 0.65f, 0.78f}, {128, 64, 1, 0.55f, 0.62f}};
 
 static Gq4Plan gq4_plan_back(int n, int k, int m, int terms)
