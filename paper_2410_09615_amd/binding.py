@@ -819,7 +819,14 @@ def slim_block_fp8_gemm_plan(n: int, k: int, m: int, dtype: torch.dtype = torch.
 
 
 # ---- 4-bit layers with a scale for each group of inputs ----
+def _sizes_in_32_bits(*sizes: int) -> None:
+    """(ctypes would take such a size modulo 2^32)"""
+    if any(not -(1 << 31) <= s < 1 << 31 for s in sizes):
+        raise ValueError(f"sizes {sizes} must be 32-bit numbers")
+
+
 def slim_group_q4_sizes(n: int, k: int, group: int = 128) -> dict:
+    _sizes_in_32_bits(n, k, group)
     c, s, z = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
     _check("slim_group_q4_sizes", lib().slim_group_q4_sizes(n, k, group, c, s, z))
     return {"codes": c.value, "scales": s.value, "zeros": z.value}
@@ -942,6 +949,7 @@ Q4_CALLS = {"gemm": 0, "gated": 1, "gemm_t": 2, "gated_backward": 3}
 
 def slim_group_q4_workspace(n: int, k: int, m: int, call: str = "gemm") -> int:
     """Bytes that a call ("gemm", "gated", "gemm_t", "gated_backward") on m tokens needs; fewer tokens can need more."""
+    _sizes_in_32_bits(n, k, m)
     out = ctypes.c_size_t()
     _check("slim_group_q4_workspace", lib().slim_group_q4_workspace(n, k, m, Q4_CALLS[call], out))
     return out.value
@@ -949,6 +957,7 @@ def slim_group_q4_workspace(n: int, k: int, m: int, call: str = "gemm") -> int:
 
 def slim_group_q4_plan(n: int, k: int, m: int, call: str = "gemm") -> dict:
     """What a call would launch (host logic; no launch): kernel "stream", "tile" or "back", outputs and tokens of a workgroup's tile, and what shares it: workgroups, or ("stream") wavefronts."""
+    _sizes_in_32_bits(n, k, m)
     out = (ctypes.c_int32 * 4)()
     _check("slim_group_q4_plan", lib().slim_group_q4_plan(n, k, m, Q4_CALLS[call], out))
     return {"kernel": ("stream", "tile", "back")[out[0]], "outputs": out[1], "tokens": out[2], "shared": out[3]}
@@ -997,22 +1006,24 @@ def slim_group_q4_gemm_t(layer: SlimGroupQ4Weight, dY: torch.Tensor, dX=None, wo
     return _q4_product("slim_group_q4_gemm_t", True, layer, dY, dX, workspace)
 
 
-def _q4_pair(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight, again: bool):
-    g, u = gate.c_ref(again), up.c_ref(again)
+def _q4_pair(gate: SlimGroupQ4Weight, g: _LayerRef, up: SlimGroupQ4Weight, u: _LayerRef):
+    """What a call is given of two layers (their references stay with the caller: a call reads them when another thread may have made new ones)."""
     return g.address, g.device, gate.codes, gate.scales, gate.zeros, u.address, u.device, up.codes, up.scales, up.zeros
 
 
 def slim_group_q4_gated(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight, X: torch.Tensor, H=None, G=None, U=None, workspace=None):
     """H [m][n] = silu(X Wg^T) * (X Wu^T) -> (H, G, U).  G, U: True for a new matrix that receives the two products (what
     slim_group_q4_gated_backward wants), or one to write; None (returned as such): not wanted.  All of X's type, any row strides, any m >= 1."""
-    ref = gate.c_ref()
+    ref, other = gate.c_ref(), up.c_ref()
     if H is None or G is True or U is True:
         new = lambda: torch.empty(X.shape[0], gate.n, dtype=X.dtype, device=gate.codes.device)
         H, G, U = new() if H is None else H, new() if G is True else G, new() if U is True else U
-    status = (_call or _calls()).q4_gated(*_q4_pair(gate, up, False), X, H, G, U, workspace)
+    status = (_call or _calls()).q4_gated(*_q4_pair(gate, ref, up, other), X, H, G, U, workspace)
     if status != SLIM_OK:
-        _q4_call("slim_group_q4_gated", gate, ref.device, X.shape[0], workspace, status,
-                 lambda again, ws: _call.q4_gated(*_q4_pair(gate, up, again), X, H, G, U, ws))
+        def call(again, ws):
+            g, u = gate.c_ref(again), up.c_ref(again)
+            return _call.q4_gated(*_q4_pair(gate, g, up, u), X, H, G, U, ws)
+        _q4_call("slim_group_q4_gated", gate, ref.device, X.shape[0], workspace, status, call)
     return H, G, U
 
 
@@ -1020,12 +1031,14 @@ def slim_group_q4_gated_backward(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight,
                                  dX=None, workspace=None):
     """Gradients through slim_group_q4_gated, its weights frozen: dH, G, U [m][n] -> (dX [m][k], dG [m][n], dU [m][n]), all of one type.
     dG may be G or dH and dU may be U or dH, but not both the same."""
-    ref = gate.c_ref()
+    ref, other = gate.c_ref(), up.c_ref()
     if dG is None or dU is None or dX is None:
         new = lambda k: torch.empty(dH.shape[0], k, dtype=dH.dtype, device=gate.codes.device)
         dG, dU, dX = new(gate.n) if dG is None else dG, new(gate.n) if dU is None else dU, new(gate.k) if dX is None else dX
-    status = (_call or _calls()).q4_backward(*_q4_pair(gate, up, False), dH, G, U, dG, dU, dX, workspace)
+    status = (_call or _calls()).q4_backward(*_q4_pair(gate, ref, up, other), dH, G, U, dG, dU, dX, workspace)
     if status != SLIM_OK:
-        _q4_call("slim_group_q4_gated_backward", gate, ref.device, dH.shape[0], workspace, status,
-                 lambda again, ws: _call.q4_backward(*_q4_pair(gate, up, again), dH, G, U, dG, dU, dX, ws))
+        def call(again, ws):
+            g, u = gate.c_ref(again), up.c_ref(again)
+            return _call.q4_backward(*_q4_pair(gate, g, up, u), dH, G, U, dG, dU, dX, ws)
+        _q4_call("slim_group_q4_gated_backward", gate, ref.device, dH.shape[0], workspace, status, call)
     return dX, dG, dU

@@ -301,3 +301,33 @@ def test_a_run_of_them(m):
     ref, mag = O.gemm(y, Vd.T)
     _check(dH, ref, _sum_bound(mag, k, y, F16), F16)
     _check_backward(dX, dG, dU, dH, want_g, want_u, Vg, Vu, F16)
+
+
+def test_gradients_of_far_rows_in_place():
+    """Rows 2^23 elements apart: dG over dH and dU over U, where a call goes token by token behind the activation's gradient."""
+    n, k, m = 40, 200, 3
+    (gate, Vg), (up, Vu) = _weights(n, k, 64, True, 1), _weights(n, k, 64, False, 2)
+    far = torch.empty(m * (1 << 23), dtype=F16, device=DEV).view(m, 1 << 23)
+    dH, G, U, dX = far[:, 1:1 + n], far[:, 100:100 + n], far[:, 201:201 + n], far[:, 300:300 + k]
+    for i, t in enumerate((dH, G, U)):
+        t.copy_(_matrix(m, n, F16, i, 2.0))
+    h, g, u = dH.clone(), G.clone(), U.clone()
+    out = B.slim_group_q4_gated_backward(gate, up, dH, G, U, dG=dH, dU=U, dX=dX)
+    assert out[0] is dX and out[1] is dH and out[2] is U and torch.equal(G, g)
+    _check_backward(dX, dH, U, h, g, u, Vg, Vu, F16)
+
+
+@pytest.mark.parametrize("m", [1, 70])
+def test_a_row_out_of_one_column_and_no_workspace_bytes(m):
+    """Layers of one input or one output: a single row's stride says nothing, and a workspace without bytes is taken where none are needed."""
+    (layer, V), (wide, Vw) = _weights(5, 1, 32, True, 1), _weights(1, 70, 32, False, 2)
+    X = _matrix(m, 1, F16, 3)
+    room = B.alloc_group_q4_workspace(layer, m)
+    assert room.numel() == 0
+    x = _np(X)
+    ref, mag = O.gemm(x, V)
+    _check(B.slim_group_q4_gemm(layer, X, workspace=room), ref, _sum_bound(mag, 1, x, F16), F16)
+    X = _matrix(70, m, F16, 4).t() if m == 1 else _matrix(m, 70, F16, 4)              # (of one token: 1 x 70 with strides 1, 1)
+    x = _np(X)
+    ref, mag = O.gemm(x, Vw)
+    _check(B.slim_group_q4_gemm(wide, X), ref, _sum_bound(mag, 70, x, F16), F16)

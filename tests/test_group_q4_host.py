@@ -175,3 +175,13 @@ def test_another_device_is_made_current_for_the_call(monkeypatch):
     assert seen == [5] and calls == [(True, None), (False, None), (False, ("room", 7, "gemm_t"))]
     with pytest.raises(B.SlimError):
         B._q4_call("slim_group_q4_gemm", None, 0, 1, "small", B.SLIM_ERR_WORKSPACE, call)
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """Not taken modulo 2^32: a matrix of 2^32 + 5 rows is not one of 5."""
+    big = (1 << 32) + 5
+    for bad in (lambda: B.slim_group_q4_sizes(big, 64), lambda: B.slim_group_q4_sizes(64, big), lambda: B.slim_group_q4_sizes(64, 64, big), lambda: B.alloc_group_q4(big, 1, device="cpu"),
+                lambda: B.slim_group_q4_workspace(64, 64, big), lambda: B.slim_group_q4_workspace(big, 64, 1), lambda: B.slim_group_q4_plan(64, 64, big),
+                lambda: B.SlimGroupQ4Weight(big, 64, 128, torch.zeros(4096, dtype=torch.uint8), torch.zeros(5, 1, dtype=torch.float16)).c_ref()):
+        with pytest.raises(ValueError):
+            bad()
