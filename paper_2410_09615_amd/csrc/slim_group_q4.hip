@@ -4,8 +4,8 @@
 //   symmetric:         s = fp16(max |w| / 7),  z = 8,              c = clamp(rint(w / s), -8, 7) + 8
 //   with zero points:  s = fp16((hi - lo) / 15),  z = rint(-lo / s),  c = clamp(rint(w / s) + z, 0, 15),   lo = min(w, 0), hi = max(w, 0)
 //   value = (c - z) s
-// Quotients in binary32.  All of these are bound by memory: quantization 4096 x 4096 fp16 17.3 us (2.5 TB/s; its 42 MB come from the last-level cache, and a wavefront's life is one
-// load, one reduction and one store), 10007 x 5003 fp32 with zero points in groups of 32 80 us (2.8 TB/s, rows at odd multiples of 4 bytes); values 10.0 and 56 us (4.2 TB/s); the activation's gradient,
+// Quotients in binary32.  All of these are bound by memory: quantization 4096 x 4096 fp16 13.1 us (3.2 TB/s; its 42 MB come from the last-level cache, all wavefronts
+// are there at once, and the life of one is a load, a reduction, codes and a store: instructions count, 17.7 us with a conversion, shift and two clamps per code and three for what is not finite), 10007 x 5003 fp32 with zero points in groups of 32 80 us (2.8 TB/s, rows at odd multiples of 4 bytes); values 10.0 and 56 us (4.2 TB/s); the activation's gradient,
 // 4096 x 11008 bf16, 73 us (6.2 TB/s).  The scale is rounded to fp16 before the codes are made, so codes are the nearest ones to the scale that is kept.
 #include <hip/hip_runtime.h>
 
@@ -43,7 +43,7 @@ __device__ __forceinline__ uint32_t over_four(uint32_t v)
 
 // a / b to the nearest, given 1 / b to the nearest: the product with it is within a step of the quotient, what it lacks is exact in one fused operation, and adding that times 1 / b rounds once
 // (Markstein's theorem; b is an fp16 number from 2^-24 to 65504, and quotients too small for it to hold are far below the 1/2 that a code begins at).  Three instructions where a division
-// takes ten: 4096 x 4096 fp16 20.8 us with divisions.
+// takes ten (3.5 us of 4096 x 4096 in fp16).
 __device__ __forceinline__ float nearest_quotient(float a, float b, float inverse)
 {
     const float q = a * inverse;
@@ -70,34 +70,57 @@ __global__ __launch_bounds__(256) void gq4_quant_kernel(Gq4QuantArgs a)
     uint8_t __attribute__((ext_vector_type(GROUPS))) points;
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-        float lo = 0.f, hi = 0.f;
-        uint32_t odd = 0;                                            // an infinity or a NaN among them
+        float lo = 0.f, hi = 0.f, span;
+        uint32_t odd;                                                // an infinity or a NaN among them
+        if constexpr (ZEROS) {
+            float none = 0.f;                                        // 0 w is a NaN for those alone
 #pragma unroll
-        for (int j = g * PER; j < (g + 1) * PER; ++j)
+            for (int j = g * PER; j < (g + 1) * PER; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                lo = fminf(lo, w[j][e]);
-                hi = fmaxf(hi, w[j][e]);
-                odd |= magnitude_bits(w[j][e]) >= 0x7f800000u;
-            }
-        lo = over_four(lo, false);
-        hi = over_four(hi, true);
-        odd = over_four(odd);
-        const float span = ZEROS ? hi - lo : fmaxf(hi, -lo);
+                for (int e = 0; e < 8; ++e) {
+                    lo = fminf(lo, w[j][e]);
+                    hi = fmaxf(hi, w[j][e]);
+                    none = __builtin_fmaf(w[j][e], 0.f, none);
+                }
+            lo = over_four(lo, false);
+            hi = over_four(hi, true);
+            odd = over_four((uint32_t)(none != 0.f));
+            span = hi - lo;
+        } else {
+            uint32_t most = 0;                                       // (magnitudes as bits: those are larger than any number's)
+#pragma unroll
+            for (int j = g * PER; j < (g + 1) * PER; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = max(most, magnitude_bits(w[j][e]));
+            most = max(most, (uint32_t)__shfl_xor((int)most, 1, kWave));
+            most = max(most, (uint32_t)__shfl_xor((int)most, 2, kWave));
+            odd = most >= 0x7f800000u;
+            span = __builtin_bit_cast(float, most);
+        }
         half_t s16 = (half_t)(span / (ZEROS ? 15.f : 7.f));
         if ((float)s16 == 0.f) s16 = span == 0.f ? (half_t)1.f : __builtin_bit_cast(half_t, (uint16_t)1);
         if ((float)s16 > 65504.f) s16 = (half_t)65504.f;
         const float s = (float)s16;
         const float inverse = 1.f / s;
         const float z = ZEROS ? fminf(fmaxf(__builtin_rintf(nearest_quotient(-lo, s, inverse)), 0.f), 15.f) : (float)kGq4Sym;
+        // rint(q) by adding 1.5 2^23, which leaves it in the low bits (what is too large for that is beyond the clamp too); z and the bits of 1.5 2^23 come in once for a dword's eight.
+        constexpr float kWhole = 12582912.f;
+        const float least = kWhole - z, largest = kWhole + 15.f - z;
+        const uint32_t rest = (uint32_t)z * 0x11111111u - 0x11111111u * 0x4b400000u;
 #pragma unroll
         for (int j = g * PER; j < (g + 1) * PER; ++j) {
-            uint32_t d = 0;
-            const int left = a.k - (cb * kGq4Cols + 32 * j + 8 * q);    // inputs there are from the piece's first on; the codes past them are 0
+            uint32_t d = rest;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float c = fminf(fmaxf(__builtin_rintf(nearest_quotient(w[j][e], s, inverse)) + z, 0.f), 15.f);
-                d |= (e < left ? (uint32_t)c : 0u) << (4 * ((e >> 1) + 4 * (e & 1)));
+                const float c = __builtin_amdgcn_fmed3f(nearest_quotient(w[j][e], s, inverse) + kWhole, least, largest);
+                d += __builtin_bit_cast(uint32_t, c) << (4 * ((e >> 1) + 4 * (e & 1)));
+            }
+            const int left = a.k - (cb * kGq4Cols + 32 * j + 8 * q);    // inputs there are from the piece's first on; the codes past them are 0
+            if (left < 8) {
+                uint32_t there = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) there |= (e < left ? 15u : 0u) << (4 * ((e >> 1) + 4 * (e & 1)));
+                d &= there;
             }
             out[j] = odd ? 0u : d;
         }
