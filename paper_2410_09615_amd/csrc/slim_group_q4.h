@@ -49,15 +49,18 @@ inline Gq4Weights gq4_weights(const slim_group_q4_layer *l)
     return Gq4Weights{l->codes, reinterpret_cast<const half_t *>(l->scales), l->zeros};
 }
 
+// 1024 as two fp16 numbers: or'd onto a nibble it makes 1024 + c.  The same 15 binades lower: (1024 + c) 2^-15, where numbers are as far apart as whole ones are here, 2^-15.
+constexpr uint32_t kGq4Bias = 0x64006400u, kGq4BiasLow = 0x28002800u;
+constexpr float kGq4Low = 0x1p-15f;
+
 // Constants that the compiler has to keep in registers: an instruction takes no two of them as literals.
 struct Gq4Masks {
     uint32_t low, high, bias;
     half2_t sixteenth;
-    __device__ __forceinline__ Gq4Masks()
+    __device__ __forceinline__ explicit Gq4Masks(uint32_t b = kGq4Bias) : bias(b)
     {
         low = 0x000f000fu;
         high = 0x00f000f0u;
-        bias = 0x64006400u;
         sixteenth = half2_t{(half_t)0.0625f, (half_t)0.0625f};
         asm volatile("" : "+s"(low), "+s"(high), "+v"(bias), "+v"(sixteenth));
     }
@@ -70,7 +73,7 @@ __device__ __forceinline__ half2_t gq4_biased(uint32_t d, const Gq4Masks &k)
     return __builtin_bit_cast(half2_t, ((E < 2 ? d : d >> 8) & (E % 2 ? k.high : k.low)) | k.bias);
 }
 // 1024 + z of two zero points in fp16 (up to 1024 the steps there are 1)
-__device__ __forceinline__ half2_t gq4_biased_zeros(uint32_t z0, uint32_t z1) { return __builtin_bit_cast(half2_t, (z1 << 16 | z0) + 0x64006400u); }
+__device__ __forceinline__ half2_t gq4_biased_zeros(uint32_t z0, uint32_t z1, uint32_t bias = kGq4Bias) { return __builtin_bit_cast(half2_t, (z1 << 16 | z0) + bias); }
 
 // c - z of nibble E of both halves, exactly; z: 1024 + the zero points.
 template <int E>

@@ -6,7 +6,7 @@
 // The wavefronts' sums meet in LDS and are added in order.
 // Bound by memory in fp16 where the layer is large: 28672 x 8192 at one token 24.0 us, 5.0 TB/s (a large copy 5.15), 2 x 28672 x 8192 gated 49, at 16 tokens 28.4.  In bf16 a pair of codes takes five instructions
 // instead of two and a half, at 16 tokens 34 to 36 us, vector instructions 60 % of the cycles.  With 48 tokens by what is issued and by the tokens' way through the L2, which every
-// workgroup takes (13824 x 5120 gated, bf16, groups of 64: 424 MB of tokens to 77 of weights, 38 us).  4096 x 4096 at one token: the call's host time, 5 us (kernel 5).
+// workgroup takes (13824 x 5120 gated, bf16, groups of 64: 424 MB of tokens to 77 of weights, 39 us).  4096 x 4096 at one token: the call's host time, 5 us (kernel 5).
 #include <hip/hip_runtime.h>
 
 #include "slim_group_q4.h"
@@ -23,7 +23,12 @@ struct Gq4StreamArgs {
     int n, k, m, cb, rb, kg;
 };
 
-// c - z of the eight codes of a dword, exactly, in the inputs' type.
+// c - z of the eight codes of a dword, exactly, in the inputs' type; in bf16 times 2^-15 (of masks and zero points that are biased so), so that a group's sum of products, at most 128 terms with
+// |c - z| up to 255, is smaller than its largest input and stays in range wherever the result does: with whole numbers tokens of 2^121 have sums beyond binary32.  (fp16's tokens end at 2^16.)
+template <class T>
+constexpr uint32_t kGq4StreamBias = __is_same(T, F16) ? kGq4Bias : kGq4BiasLow;
+template <class T>
+constexpr float kGq4StreamLow = __is_same(T, F16) ? 1.f : kGq4Low;
 template <class T>
 __device__ __forceinline__ typename Gq4Vec<T>::v8 gq4_whole(uint32_t d, const Gq4Masks &k, half2_t z0, half2_t z1)
 {
@@ -32,7 +37,7 @@ __device__ __forceinline__ typename Gq4Vec<T>::v8 gq4_whole(uint32_t d, const Gq
         const half2_t c = gq4_less_zeros<decltype(ec)::value>(d, k, z0, z1);
         if constexpr (__is_same(T, F16))
             v[decltype(ec)::value] = __builtin_bit_cast(uint32_t, c);
-        else                                                          // (whole numbers below 256: their first 16 bits in binary32)
+        else                                                          // (whole numbers below 256 times 2^-15: their first 16 bits in binary32)
             v[decltype(ec)::value] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, (float)c[1]), __builtin_bit_cast(uint32_t, (float)c[0]), 0x07060302u);
     });
     return __builtin_bit_cast(typename Gq4Vec<T>::v8, v);
@@ -67,7 +72,7 @@ __global__ __launch_bounds__(THREADS) void gq4_stream_kernel(Gq4StreamArgs a)
     constexpr int PAIRS = GATED ? FR / 2 : FR;
     const int rb0 = (int)blockIdx.x * PAIRS;
     const int whole = a.k / kGq4Cols, share = (whole + S - 1) / S, first = w * share, end = min(first + share, whole);
-    const Gq4Masks masks;
+    const Gq4Masks masks(kGq4StreamBias<T>);
 
     typedef Gq4StreamLds<FR, TB> Lds;
     uint8_t *const own = lds + w * Lds::bytes;
@@ -158,10 +163,10 @@ __global__ __launch_bounds__(THREADS) void gq4_stream_kernel(Gq4StreamArgs a)
 #pragma unroll
             for (int f = 0; f < FR; ++f) {
                 const uint8_t *table = own + Lds::scales + f * Lds::table;
-                s[f] = (float)*reinterpret_cast<const half_t *>(table + r * Lds::scale_row + (at + g) * 2);
+                s[f] = (float)*reinterpret_cast<const half_t *>(table + r * Lds::scale_row + (at + g) * 2) * (1.f / kGq4StreamLow<T>);
                 const uint32_t zp = table[16 * Lds::scale_row + r * Lds::zero_row + at + g];
-                z0[f] = gq4_biased_zeros(zp, zp);
-                z1[f] = z0[f] - half2_t{(half_t)960.f, (half_t)960.f};
+                z0[f] = gq4_biased_zeros(zp, zp, kGq4StreamBias<T>);
+                z1[f] = z0[f] - half2_t{(half_t)(960.f * kGq4StreamLow<T>), (half_t)(960.f * kGq4StreamLow<T>)};
 #pragma unroll
                 for (int t = 0; t < TB; ++t) p[f][t] = float4_t{0.f, 0.f, 0.f, 0.f};
             }
