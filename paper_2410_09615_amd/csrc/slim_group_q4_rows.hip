@@ -321,6 +321,12 @@ __global__ __launch_bounds__(KG *WR *kWave, 2) void gq4_rows_kernel(Gq4RowsArgs 
                     vec8 af[AF], bf[BF];
                     read(own, decltype(kkc)::value, bf);
                     number(v, sc, kkc, af);
+                    // (past the layer's inputs there are no weights: what their codes of 0 stand for can be beyond fp16, and infinite times the tokens' zeros is a NaN)
+                    const int from = 32 * decltype(kkc)::value + 16 * e + 8 * (lane >> 5);
+#pragma unroll
+                    for (int i = 0; i < AF; ++i)
+#pragma unroll
+                        for (int z = 0; z < 8; ++z) af[i][z] = from + z < left ? af[i][z] : (E)0.f;
                     multiply(af, bf);
                 });
             }
