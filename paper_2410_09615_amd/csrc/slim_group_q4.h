@@ -83,8 +83,33 @@ __device__ __forceinline__ half2_t gq4_less_zeros(uint32_t d, const Gq4Masks &k,
     return E % 2 ? __builtin_elementwise_fma(c, k.sixteenth, -z_sixteenth) : c - z;
 }
 
+// ---- scales that fp16 weights cannot have ----
+// (c - z) s reaches 255 x 65504, fp16 ends at 65504.  Where weights are rounded to fp16, groups whose scale is 256 or more are left out (a scale of 0; below that values stay below 256 x 255 =
+// 65280), and where a workgroup has met one it goes over its share once more for those alone, with weights and inputs as sums of two bf16 numbers (16 bits of a weight, all 11 of an input), whose
+// four products are added to the same sums.  Scales that are not finite stay with the others.  What it costs where there are none: six instructions for four scales, and a barrier.
+__device__ __forceinline__ bool gq4_large(uint32_t h) { return (h & 0x7fffu) - 0x5c00u < 0x2000u; }             // 256 to 65504, as bits of fp16
+// the scale if it is one of these (rest) or if it is none, and 0 otherwise
+__device__ __forceinline__ uint32_t gq4_scale_of(uint32_t h, bool rest) { return gq4_large(h) == rest ? h : 0u; }
+// whether one of the four scales is large or not finite
+__device__ __forceinline__ bool gq4_any_large(uint2_t s)
+{
+    return ((((s[0] & 0x7fff7fffu) + 0x24002400u) | ((s[1] & 0x7fff7fffu) + 0x24002400u)) & 0x80008000u) != 0;
+}
+constexpr int kGq4Flags = 64;                                                   // bytes of LDS behind the windows: one number for each wavefront
+// Whether any of the workgroup's `waves` wavefronts has it.
+__device__ __forceinline__ bool gq4_any_wave(bool mine, uint8_t *flags, int wave, int waves)
+{
+    uint32_t *const f = reinterpret_cast<uint32_t *>(flags);
+    const bool any = __ballot(mine) != 0;
+    if ((threadIdx.x & (kWave - 1)) == 0) f[wave] = any;
+    __syncthreads();
+    uint32_t all = 0;
+    for (int i = 0; i < waves; ++i) all |= f[i];
+    return __builtin_amdgcn_readfirstlane((int)all) != 0;
+}
+
 // What turns codes into values (c - z) s, for the two halves (of one group or of two).
-//   fp16: c - z exactly, and one rounding of the product to fp16.
+//   fp16: c - z exactly, and one rounding of the product to fp16 (of scales below 256).
 //   bf16: (1024 + c) s - (1024 + z) s by one fused operation in binary32, exact since a code, a zero point and a scale have 23 bits between them; one rounding.
 template <class T>
 struct Gq4Pair;
@@ -151,6 +176,20 @@ __device__ __forceinline__ float4_t gq4_mma16(Gq4Vec<F16>::v8 a, Gq4Vec<F16>::v8
 __device__ __forceinline__ float4_t gq4_mma16(Gq4Vec<BF16>::v8 a, Gq4Vec<BF16>::v8 b, float4_t c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// The first (0) or second (1) bf16 number of the two whose sum is v to 16 bits, as bits; of 8 fp16 numbers.
+__device__ __forceinline__ uint32_t gq4_part_of(float v, int part)
+{
+    const uint32_t first = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
+    return part ? (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)(v - __builtin_bit_cast(float, first))) : first >> 16;
+}
+__device__ __forceinline__ Gq4Vec<BF16>::v8 gq4_part_of(Gq4Vec<F16>::v8 v, int part)
+{
+    uint4_t out;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = gq4_part_of((float)v[2 * e], part) | gq4_part_of((float)v[2 * e + 1], part) << 16;
+    return __builtin_bit_cast(Gq4Vec<BF16>::v8, out);
 }
 
 // The 16-byte pieces of an LDS row of 64 values are put in another order in each of eight rows, so that the lanes of a read or write find all banks; the

@@ -123,7 +123,8 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
         }
     };
     // the first `there` rows are there: the others are no terms of the sum
-    auto put_window = [&](int w, int there) {
+    bool large = false;                                                          // (fp16) whether there was a scale whose group is left out: gq4_large
+    auto put_window = [&](int w, int there, bool rest) {
         uint8_t *const t = tables + (w & 1) * TABLE;
         int own_tid = tid;
         asm volatile("" : "+v"(own_tid));
@@ -132,7 +133,12 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
         for (int i = 0; i < ITEMS; ++i) {
             const int item = own_tid + i * THREADS, row = item / SPAN, g = item % SPAN;
             if (item >= 64 * SPAN) continue;
-            *reinterpret_cast<half_t *>(t + (g * 64 + row) * 2) = row < there ? ahead.s[i] : (half_t)0.f;
+            uint32_t h = row < there ? __builtin_bit_cast(uint16_t, ahead.s[i]) : 0;
+            if constexpr (__is_same(T, F16)) {
+                large |= gq4_large(h);
+                h = gq4_scale_of(h, rest);
+            }
+            *reinterpret_cast<uint16_t *>(t + (g * 64 + row) * 2) = (uint16_t)h;
             t[8 * 64 * 2 + g * 64 + row] = points ? (uint8_t)ahead.z[i] : (uint8_t)kGq4Sym;
         }
     };
@@ -167,6 +173,20 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
             const uint2_t out = {v01.template value<h>(d01, masks), v23.template value<h>(d23, masks)};
             *reinterpret_cast<uint2_t *>(to + (wl_at[i] ^ (uint32_t)(e * 16)) + e * 128) = out;
         });
+    };
+
+    // (fp16) a weight task's first or second part, of scales that fp16 weights cannot have
+    auto put_w_rest = [&](const Share &v, const Scales &sc, int i, int part, uint8_t *to) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            uint32_t b[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int c = (int)(v.w[i][r] >> (4 * (e >> 1) + 16 * (e & 1)) & 15u), z = (int)(sc.z[i] >> (8 * r) & 255u);
+                b[r] = gq4_part_of((float)(c - z) * (float)sc.s[i][r], part);
+            }
+            *reinterpret_cast<uint2_t *>(to + (wl_at[i] ^ (uint32_t)(e * 16)) + e * 128) = uint2_t{b[0] | b[1] << 16, b[2] | b[3] << 16};
+        }
     };
 
     float16_t acc[AF][BF];
@@ -225,9 +245,9 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
         Scales sc;
         load_window_of(0);
         fetch(pieces[0], 0);
-        put_window(0, 64);
+        put_window(0, 64, false);
         load_window_of(1);
-        put_window(1, 64);
+        put_window(1, 64, false);
         load_window_of(2);
         __syncthreads();
         read_scales(sc, 0);
@@ -256,7 +276,7 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
                     read(kk < 3 ? from : to, (kk + 1) & 3, af[(kk + 1) & 1], bf[(kk + 1) & 1]);
                     // (the window of step s + 1, in registers by now, is left by all; that of s + 2 is there, and the one after it takes its place past the barrier)
                     if constexpr (kk == 0) {
-                        put_window(s, 64);
+                        put_window(s, 64, false);
                         load_window_of(s + 3);
                     }
                     if constexpr (kk == 3) read_scales(sc, s);
@@ -286,42 +306,94 @@ __global__ __launch_bounds__(KG *WR *WT *kWave, 2) void gq4_back_kernel(Gq4BackA
             }
         }
     }
-    if (a.n % 64 && (int)blockIdx.y == a.split.splits - 1) {
+    // ---- pieces without overlap, by the first group of wavefronts ----
+    const int tails = a.n % 64 && (int)blockIdx.y == a.split.splits - 1 ? a.terms : 0;
+    // a piece's inputs element by element, and its codes
+    auto stage_x = [&](Share &v, int term, int at, auto &&of) {
+        const E *x = static_cast<const E *>(term ? a.x[1] : a.x[0]);
+        const int64_t ld = term ? a.x_ld[1] : a.x_ld[0];
+#pragma unroll
+        for (int i = 0; i < XTASKS; ++i) {
+            const E *row = x + ((int64_t)t0 + x_at[i]) * ld;
+            const int c = at + (tid & 7) * 8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v.x[i][e] = c + e < a.n ? of(row[c + e]) : (E)0.f;
+            put_x(v, i, own, true);
+        }
+    };
+    auto stage_w = [&](Share &v, int i, int at) {
+        const int rl = (gw + i * (WR * WT)) & 3;
+        fetch_w(v, i, (min((at >> 4) + rl, a.rb - 1) - rl) * 16);                // (blocks of rows past the last are not there)
+    };
+    // rows that do not fill a piece, of each layer
+    for (int term = 0; term < tails; ++term) {
         const int at = whole * 64;
-        for (int term = 0; term < a.terms; ++term) {
-            use_term(term);
-            load_window(term, at);
-            __syncthreads();                                                     // (nobody reads from LDS any more)
-            put_window(0, a.n - at);
-            __syncthreads();
-            if (group == 0) {
-                const E *x = static_cast<const E *>(term ? a.x[1] : a.x[0]);
-                const int64_t ld = term ? a.x_ld[1] : a.x_ld[0];
-                Share &v = pieces[0];
-                Scales sc;
-                read_scales(sc, 0);
+        use_term(term);
+        load_window(term, at);
+        __syncthreads();                                                         // (nobody reads from LDS any more)
+        put_window(0, a.n - at, false);
+        __syncthreads();
+        if (group == 0) {
+            Share &v = pieces[0];
+            Scales sc;
+            read_scales(sc, 0);
+            stage_x(v, term, at, [](E e) { return e; });
 #pragma unroll
-                for (int i = 0; i < XTASKS; ++i) {
-                    const E *row = x + ((int64_t)t0 + x_at[i]) * ld;
-                    const int c = at + (tid & 7) * 8;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v.x[i][e] = c + e < a.n ? row[c + e] : (E)0.f;
-                    put_x(v, i, own, true);
-                }
-#pragma unroll
-                for (int i = 0; i < WTASKS; ++i) {
-                    const int rl = (gw + i * (WR * WT)) & 3;
-                    fetch_w(v, i, (min((at >> 4) + rl, a.rb - 1) - rl) * 16);    // (blocks of rows past the last are not there)
-                    static_for<4>([&](auto h) { put_w(v, sc, i, h, own); });
-                }
+            for (int i = 0; i < WTASKS; ++i) {
+                stage_w(v, i, at);
+                static_for<4>([&](auto h) { put_w(v, sc, i, h, own); });
             }
-            __syncthreads();
-            if (group == 0) {
+        }
+        __syncthreads();
+        if (group == 0) {
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) {
-                    vec8 af[AF], bf[BF];
-                    read(own, kk, af, bf);
-                    multiply(af, bf);
+            for (int kk = 0; kk < 4; ++kk) {
+                vec8 af[AF], bf[BF];
+                read(own, kk, af, bf);
+                multiply(af, bf);
+            }
+        }
+    }
+    if constexpr (__is_same(T, F16)) {
+        // groups that were left out: pieces of the share, and what does not fill one
+        if (gq4_any_wave(large, lds + Lds::bytes, wave, KG * WR * WT)) {
+            const int full = max(steps, 0);
+            for (int p = 0; p < full + tails; ++p) {
+                const int term = p < full ? (begin + p >= whole ? 1 : 0) : p - full, at = p < full ? (begin + p - term * whole) * 64 : whole * 64;
+                use_term(term);
+                load_window(term, at);
+                __syncthreads();
+                put_window(0, min(64, a.n - at), true);
+                for (int part = 0; part < 2; ++part) {
+                    __syncthreads();
+                    if (group == 0) {
+                        Share &v = pieces[0];
+                        Scales sc;
+                        read_scales(sc, 0);
+                        // (an infinite input has had its part: times the scales that are 0 now it would be a NaN)
+                        if (part == 0) stage_x(v, term, at, [](E e) { return __builtin_isfinite((float)e) ? e : (E)0.f; });
+#pragma unroll
+                        for (int i = 0; i < WTASKS; ++i) {
+                            stage_w(v, i, at);
+                            put_w_rest(v, sc, i, part, own);
+                        }
+                    }
+                    __syncthreads();
+                    if (group == 0) {
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk) {
+                            vec8 af[AF], bf[BF];
+                            read(own, kk, af, bf);
+#pragma unroll
+                            for (int t = 0; t < BF; ++t)
+#pragma unroll
+                                for (int other = 0; other < 2; ++other) {
+                                    const Gq4Vec<BF16>::v8 x = gq4_part_of(bf[t], other);
+#pragma unroll
+                                    for (int i = 0; i < AF; ++i) acc[i][t] = gq4_mma32(__builtin_bit_cast(Gq4Vec<BF16>::v8, af[i]), x, acc[i][t]);
+                                }
+                        }
+                    }
                 }
             }
         }
@@ -420,7 +492,7 @@ template <class T, int SHIFT, int SHAPE, int KG, int P, int WR, int WT, int AF, 
 static int launch_gq4_back_of(Gq4BackArgs a, hipStream_t st)
 {
     constexpr int THREADS = KG * WR * WT * kWave, BO = 32 * AF * WR, BT = 32 * BF * WT;
-    constexpr size_t RING = Gq4BackLds<KG, BO, BT>::bytes, SUMS = (size_t)BO * BT * (KG > 1 ? 4 : 2), LDS = RING > SUMS ? RING : SUMS;
+    constexpr size_t RING = Gq4BackLds<KG, BO, BT>::bytes + kGq4Flags, SUMS = (size_t)BO * BT * (KG > 1 ? 4 : 2), LDS = RING > SUMS ? RING : SUMS;
     static_assert(LDS * kBackShapes[SHAPE].per_cu <= 160 * 1024 && kBackShapes[SHAPE].outs == BO && kBackShapes[SHAPE].toks == BT, "the table's tile");
     a.tiles_o = (int)(((int64_t)a.k + BO - 1) / BO);
     a.tiles_t = (int)(((int64_t)a.m + BT - 1) / BT);

@@ -148,7 +148,8 @@ __global__ __launch_bounds__(KG *WR *kWave, 2) void gq4_rows_kernel(Gq4RowsArgs 
             }
         }
     };
-    auto put_window = [&](int w) {
+    bool large = false;                                                        // (fp16) whether there was a scale whose group is left out: gq4_large
+    auto put_window = [&](int w, bool rest) {
         uint8_t *const t = tables + (w & 1) * TABLE;
         int own_tid = tid;
         asm volatile("" : "+v"(own_tid));
@@ -156,6 +157,16 @@ __global__ __launch_bounds__(KG *WR *kWave, 2) void gq4_rows_kernel(Gq4RowsArgs 
         for (int i = 0; i < ITEMS; ++i) {
             const int item = own_tid + i * THREADS, row = item / 2, g = 8 * w + 4 * (item % 2), down = g - max(min(g, a.kg - 4), 0);
             const bool points = (GATED && (row & 32) ? a.w[1].zeros : a.w[0].zeros) != nullptr;
+            if constexpr (__is_same(T, F16)) {
+                if (rest || gq4_any_large(ahead.s[i])) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t at = 16 * (e & 1), h = ahead.s[i][e / 2] >> at & 0xffffu;
+                        large |= gq4_large(h);
+                        ahead.s[i][e / 2] = (ahead.s[i][e / 2] & ~(0xffffu << at)) | gq4_scale_of(h, rest) << at;
+                    }
+                }
+            }
             // (groups that are not there, whose places get anything, may be all four)
             const uint64_t s = (uint64_t)ahead.s[i][1] << 32 | ahead.s[i][0];
             *reinterpret_cast<uint64_t *>(t + row * 24 + (item % 2) * 8) = s >> (16 * (down & 3));
@@ -221,6 +232,22 @@ __global__ __launch_bounds__(KG *WR *kWave, 2) void gq4_rows_kernel(Gq4RowsArgs 
 #pragma unroll
             for (int i = 0; i < AF; ++i) acc[i][t] = gq4_mma32(af[i], bf[t], acc[i][t]);
     };
+    // (fp16) the first or second part of the numbers of dword kk, of scales that fp16 weights cannot have
+    auto number_rest = [&](const Codes &v, const Scales &sc, auto kkc, int part, Gq4Vec<BF16>::v8 (&af)[AF]) {
+        constexpr int kk = decltype(kkc)::value, g = kk / PER;
+#pragma unroll
+        for (int i = 0; i < AF; ++i) {
+            const float s = (float)__builtin_bit_cast(half_t, (uint16_t)(sc.s[i][g / 2] >> (16 * (g & 1))));
+            const int z = (int)(NG == 1 ? sc.z[i] : sc.z[i] >> (8 * g) & 255u);
+            uint4_t out;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t d = v.c[i][kk] >> (4 * e);
+                out[e] = gq4_part_of((float)((int)(d & 15u) - z) * s, part) | gq4_part_of((float)((int)(d >> 16 & 15u) - z) * s, part) << 16;
+            }
+            af[i] = __builtin_bit_cast(Gq4Vec<BF16>::v8, out);
+        }
+    };
 
     if (steps > 0) {
         // (past the group's last step the last is fetched again; a group without steps has the layer's first)
@@ -234,9 +261,9 @@ __global__ __launch_bounds__(KG *WR *kWave, 2) void gq4_rows_kernel(Gq4RowsArgs 
         for (int i = 0; i < XTASKS; ++i) fetch_x(x[0], i, step_of(0));
 #pragma unroll
         for (int i = 0; i < RW; ++i) fetch_w(w[i], step_of(i));
-        put_window(window);
+        put_window(window, false);
         load_window(window + 1);
-        put_window(window + 1);
+        put_window(window + 1, false);
         load_window(window + 2);
 #pragma unroll
         for (int i = 0; i < XTASKS; ++i) put_x(x[0], i, own, KG == 1 || mine > 0);
@@ -260,7 +287,7 @@ __global__ __launch_bounds__(KG *WR *kWave, 2) void gq4_rows_kernel(Gq4RowsArgs 
                 // barrier), and the one after it takes its place; a window has four steps at least.
                 if (window_of(step) != window) {
                     window = window_of(step);
-                    put_window(window + 1);
+                    put_window(window + 1, false);
                     load_window(window + 2);
                 }
                 static_for<4>([&](auto kkc) {
@@ -292,25 +319,30 @@ __global__ __launch_bounds__(KG *WR *kWave, 2) void gq4_rows_kernel(Gq4RowsArgs 
             }
         }
     }
-    if (whole < a.cb && (int)blockIdx.y == a.split.splits - 1) {
-        // inputs that end inside a block: its two halves, tokens element by element, without overlap
-        const int left = a.k - whole * kGq4Cols, w = window_of(2 * whole);
+    // ---- steps without overlap, by the first group of wavefronts ----
+    const int tail = whole < a.cb && (int)blockIdx.y == a.split.splits - 1 ? 2 : 0;
+    // a step's tokens, element by element
+    auto stage_x = [&](int step, auto &&of) {
+        const int left = a.k - (step >> 1) * kGq4Cols;
+#pragma unroll
+        for (int i = 0; i < XTASKS; ++i) {
+            const int row = (tid + i * THREADS) >> 3, p = tid & 7, c = 32 * (p >> 1) + 16 * (step & 1) + 8 * (p & 1);
+            const E *at = static_cast<const E *>(a.x) + (int64_t)min(t0 + row, a.m - 1) * a.x_ld + (int64_t)(step >> 1) * kGq4Cols + c;
+            Tokens v;
+#pragma unroll
+            for (int z = 0; z < 8; ++z) v.x[i][z] = c + z < left ? of(at[z]) : (E)0.f;
+            put_x(v, i, own, true);
+        }
+    };
+    if (tail) {
+        // inputs that end inside a block: its two halves
+        const int w = window_of(2 * whole);
         load_window(w);
         __syncthreads();                                                      // (nobody reads from LDS any more)
-        put_window(w);
+        put_window(w, false);
         for (int e = 0; e < 2; ++e) {
             __syncthreads();
-            if (group == 0) {
-#pragma unroll
-                for (int i = 0; i < XTASKS; ++i) {
-                    const int row = (tid + i * THREADS) >> 3, p = tid & 7, c = 32 * (p >> 1) + 16 * e + 8 * (p & 1);
-                    const E *at = static_cast<const E *>(a.x) + (int64_t)min(t0 + row, a.m - 1) * a.x_ld + (int64_t)whole * kGq4Cols + c;
-                    Tokens v;
-#pragma unroll
-                    for (int z = 0; z < 8; ++z) v.x[i][z] = c + z < left ? at[z] : (E)0.f;
-                    put_x(v, i, own, true);
-                }
-            }
+            if (group == 0) stage_x(2 * whole + e, [](E v) { return v; });
             __syncthreads();
             if (group == 0) {
                 Codes v;
@@ -321,14 +353,45 @@ __global__ __launch_bounds__(KG *WR *kWave, 2) void gq4_rows_kernel(Gq4RowsArgs 
                     vec8 af[AF], bf[BF];
                     read(own, decltype(kkc)::value, bf);
                     number(v, sc, kkc, af);
-                    // (past the layer's inputs there are no weights: what their codes of 0 stand for can be beyond fp16, and infinite times the tokens' zeros is a NaN)
-                    const int from = 32 * decltype(kkc)::value + 16 * e + 8 * (lane >> 5);
-#pragma unroll
-                    for (int i = 0; i < AF; ++i)
-#pragma unroll
-                        for (int z = 0; z < 8; ++z) af[i][z] = from + z < left ? af[i][z] : (E)0.f;
                     multiply(af, bf);
                 });
+            }
+        }
+    }
+    if constexpr (__is_same(T, F16)) {
+        // groups that were left out
+        if (gq4_any_wave(large, lds + Lds::bytes, wave, KG * WR)) {
+            for (int step = min(begin, end); step < end + tail; ++step) {
+                const int w = window_of(step);
+                load_window(w);
+                __syncthreads();
+                put_window(w, true);
+                // (an infinite token has had its part: times the scales that are 0 now it would be a NaN)
+                if (group == 0) stage_x(step, [](E v) { return __builtin_isfinite((float)v) ? v : (E)0.f; });
+                __syncthreads();
+                if (group == 0) {
+                    Codes v;
+                    fetch_w(v, step);
+                    Scales sc;
+                    read_scales(sc, step);
+                    static_for<4>([&](auto kkc) {
+                        vec8 bf[BF];
+                        read(own, decltype(kkc)::value, bf);
+#pragma unroll
+                        for (int part = 0; part < 2; ++part) {
+                            Gq4Vec<BF16>::v8 af[AF];
+                            number_rest(v, sc, kkc, part, af);
+#pragma unroll
+                            for (int t = 0; t < BF; ++t)
+#pragma unroll
+                                for (int other = 0; other < 2; ++other) {
+                                    const Gq4Vec<BF16>::v8 x = gq4_part_of(bf[t], other);
+#pragma unroll
+                                    for (int i = 0; i < AF; ++i) acc[i][t] = gq4_mma32(af[i], x, acc[i][t]);
+                                }
+                        }
+                    });
+                }
             }
         }
     }
@@ -421,7 +484,7 @@ template <class T, bool GATED, int SHIFT, int SHAPE, int KG, int WR, int BF, int
 static int launch_gq4_rows_of(Gq4RowsArgs a, hipStream_t st)
 {
     constexpr int THREADS = KG * WR * kWave, BO = 64 * WR, BT = 32 * BF;
-    constexpr size_t OUT = (size_t)BO * BT * 2 / (GATED ? 2 : 1), SUMS = KG > 1 ? (size_t)BO * BT * 4 : 0, RING = Gq4RowsLds<KG, BO, BT>::bytes;
+    constexpr size_t OUT = (size_t)BO * BT * 2 / (GATED ? 2 : 1), SUMS = KG > 1 ? (size_t)BO * BT * 4 : 0, RING = Gq4RowsLds<KG, BO, BT>::bytes + kGq4Flags;
     constexpr size_t LDS = RING > OUT ? (RING > SUMS ? RING : SUMS) : OUT > SUMS ? OUT : SUMS;
     static_assert(LDS * kRowShapes[SHAPE].per_cu <= 160 * 1024 && kRowShapes[SHAPE].outs == BO && kRowShapes[SHAPE].toks == BT, "the table's tile");
     const int wide = GATED ? BO / 2 : BO;

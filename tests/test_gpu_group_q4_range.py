@@ -8,7 +8,7 @@ import torch
 
 from oracle import group_q4 as O
 from paper_2410_09615_amd import binding as B
-from tests.test_gpu_group_q4 import DEV, _check, _matrix, _np, _sum_bound, _weights
+from tests.test_gpu_group_q4 import DEV, _check, _check_backward, _check_gated, _matrix, _np, _sum_bound, _weights
 
 pytestmark = pytest.mark.gpu
 F16, BF16 = torch.float16, torch.bfloat16
@@ -51,3 +51,61 @@ def test_inputs_that_do_not_exist_have_no_part(m, n, k, group):
         _, G, U = B.slim_group_q4_gated(layer, layer, X, G=True, U=True)
         _check(G, ref, _sum_bound(mag, k, x, F16), F16)
         assert torch.equal(G, U)
+
+
+def _wide(n, k, group, seed, most):
+    """Scales of all sizes, each with one of 256 or more among small ones, and zero points of any byte."""
+    g = np.random.default_rng(seed)
+    codes = g.integers(0, 16, (n, k), dtype=np.uint8)
+    shape = (n, O.groups(k, group))
+    scales = (2.0 ** g.uniform(-12, np.log2(most), shape)).astype(np.float16)
+    scales[::3] = (2.0 ** g.uniform(-12, -6, scales[::3].shape)).astype(np.float16)      # (rows without a large one)
+    scales *= np.where(g.random(shape) < 0.3, -1, 1).astype(np.float16)
+    points = g.integers(0, 256, shape, dtype=np.uint8)
+    layer = B.SlimGroupQ4Weight(n, k, group, B.slim_group_q4_tile(torch.from_numpy(codes).to(DEV)), torch.from_numpy(scales).to(DEV), torch.from_numpy(points).to(DEV))
+    return layer, O.values(codes, scales, points, group)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("m,n,k", [(5, 300, 700), (200, 200, 700), (200, 200, 2600), (130, 4099, 1000), (513, 8200, 200), (70, 2050, 4100), (400, 200, 8200), (600, 700, 2600)])
+def test_weights_beyond_fp16(m, n, k, group, dtype):
+    """(c - z) s to 255 x 2000, far beyond 65504: finite, and within half a step of it, in every kernel."""
+    (one, Va), (two, Vb) = _wide(n, k, group, 1, 2000), _wide(n, k, group, 2, 2000)
+    assert np.abs(Va).max() > 4e5
+    X, dY = _matrix(m, k, dtype, 3, 2.0 ** -19), _matrix(m, n, dtype, 4, 2.0 ** -14)
+    x, y = _np(X), _np(dY)
+    ref, mag = O.gemm(x, Va)
+    _check(B.slim_group_q4_gemm(one, X), ref, _sum_bound(mag, k, x, dtype), dtype)
+    _check_gated(*B.slim_group_q4_gated(one, two, X, G=True, U=True), x, Va, Vb, k, dtype)
+    ref, mag = O.gemm(y, Va.T)
+    _check(B.slim_group_q4_gemm_t(one, dY), ref, _sum_bound(mag, n, y, dtype), dtype)
+    G, U = _matrix(m, n, dtype, 5), _matrix(m, n, dtype, 6)
+    _check_backward(*B.slim_group_q4_gated_backward(one, two, dY, G, U), dY, G, U, Va, Vb, dtype)
+
+
+@pytest.mark.parametrize("m", [70, 300])
+def test_what_is_not_finite_beside_weights_beyond_fp16(m):
+    """An infinite input: rows without large scales have what the definition has, the others are not finite, other tokens' results are as without it.  A scale of NaN: its row's results and its group's
+    gradients, no others."""
+    n, k = 300, 640
+    layer, V = _wide(n, k, 64, 1, 2000)
+    X, dY = _matrix(m, k, F16, 2, 2.0 ** -13), _matrix(m, n, F16, 3, 2.0 ** -14)
+    y, x = B.slim_group_q4_gemm(layer, X).clone(), B.slim_group_q4_gemm_t(layer, dY).clone()
+    bad = X.clone()
+    bad[3, 100] = float("inf")
+    got, others = B.slim_group_q4_gemm(layer, bad), torch.arange(m, device=DEV) != 3
+    assert torch.equal(got[others], y[others]) and not bool(torch.isfinite(got[3]).any())
+    small = torch.arange(n) % 3 == 0                                  # (rows of _wide without a large scale)
+    want = torch.where(torch.from_numpy(V[:, 100]) > 0, float("inf"), -float("inf"))
+    want[torch.from_numpy(V[:, 100]) == 0] = float("nan")
+    assert torch.equal(got[3].float().cpu()[small].nan_to_num(nan=7.0), want[small].nan_to_num(nan=7.0))
+    bad = dY.clone()
+    bad[3, 0] = -float("inf")
+    got = B.slim_group_q4_gemm_t(layer, bad)
+    assert torch.equal(got[others], x[others]) and not bool(torch.isfinite(got[3]).any())
+    layer.scales[n - 1, 4] = float("nan")
+    got = B.slim_group_q4_gemm(layer, X)
+    assert bool(torch.isnan(got[:, n - 1]).all()) and torch.equal(got[:, :n - 1], y[:, :n - 1])
+    got = B.slim_group_q4_gemm_t(layer, dY)
+    assert bool(torch.isnan(got[:, 256:320]).all()) and torch.equal(got[:, :256], x[:, :256]) and torch.equal(got[:, 320:], x[:, 320:])
