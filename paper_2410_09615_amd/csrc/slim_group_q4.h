@@ -249,8 +249,23 @@ inline Gq4Plan gq4_plan(const Gq4Shape (&shapes)[N], int outs, int m, int steps,
 
 int gq4_launch_finish(const Gq4Split &p, int m, int outs, bool gated, void *const (&y)[3], const int64_t (&y_ld)[3], int32_t dtype, hipStream_t st);
 
-// silu(g) = g sigma(g)
-__device__ __forceinline__ float gq4_sigma(float g) { return 1.f / (1.f + __expf(-g)); }
+// sigma(g) = 1 / (1 + exp(-g)) as a product of two factors, exp(-|g| / 2) each below 0: what silu is multiplied by may be as large as sigma is small, and each of the two is in binary32's range as long
+// as a result in bf16 is (1 / (1 + exp(-g)) itself is 0 from -88.7 on, where silu(g) u has values down to -190).  An exponential of a quarter, squared twice: the instruction gives no subnormal numbers.
+struct Gq4Sigma {
+    float s, h;
+    __device__ __forceinline__ explicit Gq4Sigma(float g)
+    {
+        const float quarter = __expf(-0.25f * __builtin_fabsf(g)), half = quarter * quarter;
+        h = g < 0.f ? half : 1.f;
+        s = h / (1.f + half * half);
+    }
+};
+// silu(g) u
+__device__ __forceinline__ float gq4_gated(float g, float u)
+{
+    const Gq4Sigma sigma(g);
+    return (g * sigma.s) * (sigma.h * u);
+}
 
 }  // namespace slim
 #endif

@@ -220,9 +220,9 @@ __global__ __launch_bounds__(256) void gq4_act_backward_kernel(Gq4ActArgs a)
         load_piece<T, 8>(static_cast<const E *>(a.U) + row * a.u_ld, at, a.n, u);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float sig = gq4_sigma(g[e]);
-            u[e] *= h[e] * (sig * (1.f + g[e] * (1.f - sig)));
-            h[e] *= g[e] * sig;
+            const Gq4Sigma sigma(g[e]);
+            u[e] = (sigma.s * (1.f + g[e] * (1.f - sigma.s * sigma.h)) * h[e]) * (sigma.h * u[e]);
+            h[e] = (g[e] * sigma.s) * (sigma.h * h[e]);
         }
         store_piece<T, 8>(static_cast<E *>(a.dG) + row * a.dg_ld, at, a.n, u);
         store_piece<T, 8>(static_cast<E *>(a.dU) + row * a.du_ld, at, a.n, h);
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(256) void gq4_finish_kernel(Gq4Split p, int m, int 
         if constexpr (GATED) {
             float h[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[e] = v[0][e] * gq4_sigma(v[0][e]) * v[1][e];
+            for (int e = 0; e < 8; ++e) h[e] = gq4_gated(v[0][e], v[1][e]);
             store_piece<T, 8>(static_cast<E *>(y0) + row * ld0, at, outs, h);
             if (y1) store_piece<T, 8>(static_cast<E *>(y1) + row * ld1, at, outs, v[0]);
             if (y2) store_piece<T, 8>(static_cast<E *>(y2) + row * ld2, at, outs, v[1]);

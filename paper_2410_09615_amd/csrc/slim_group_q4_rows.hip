@@ -470,10 +470,7 @@ __global__ __launch_bounds__(KG *WR *kWave, 2) void gq4_rows_kernel(Gq4RowsArgs 
         }
     };
     if constexpr (GATED) {
-        leave(a.y[0], a.y_ld[0], [&](int i, int t, int e) {
-            const float g = acc[i][t][e];
-            return g * gq4_sigma(g) * acc[i + 1][t][e];
-        });
+        leave(a.y[0], a.y_ld[0], [&](int i, int t, int e) { return gq4_gated(acc[i][t][e], acc[i + 1][t][e]); });
         if (a.y[1]) leave(a.y[1], a.y_ld[1], [&](int i, int t, int e) { return acc[i][t][e]; });
         if (a.y[2]) leave(a.y[2], a.y_ld[2], [&](int i, int t, int e) { return acc[i + 1][t][e]; });
     } else

@@ -262,7 +262,7 @@ __global__ __launch_bounds__(THREADS) void gq4_stream_kernel(Gq4StreamArgs a)
                 const int64_t tok = t0 + 16 * t + 4 * q + e;
                 if (tok < a.m) {
                     if constexpr (GATED) {
-                        static_cast<E *>(a.y[0])[tok * a.y_ld[0] + row] = (E)(v[e] * gq4_sigma(v[e]) * u[e]);
+                        static_cast<E *>(a.y[0])[tok * a.y_ld[0] + row] = (E)gq4_gated(v[e], u[e]);
                         if (a.y[1]) static_cast<E *>(a.y[1])[tok * a.y_ld[1] + row] = (E)v[e];
                         if (a.y[2]) static_cast<E *>(a.y[2])[tok * a.y_ld[2] + row] = (E)u[e];
                     } else

@@ -8,7 +8,7 @@ import torch
 
 from oracle import group_q4 as O
 from paper_2410_09615_amd import binding as B
-from tests.test_gpu_group_q4 import DEV, _check, _check_backward, _check_gated, _matrix, _np, _sum_bound, _weights
+from tests.test_gpu_group_q4 import DEV, HALF, U24, _check, _check_backward, _check_gated, _matrix, _np, _sum_bound, _weights
 
 pytestmark = pytest.mark.gpu
 F16, BF16 = torch.float16, torch.bfloat16
@@ -109,3 +109,53 @@ def test_what_is_not_finite_beside_weights_beyond_fp16(m):
     assert bool(torch.isnan(got[:, n - 1]).all()) and torch.equal(got[:, :n - 1], y[:, :n - 1])
     got = B.slim_group_q4_gemm_t(layer, dY)
     assert bool(torch.isnan(got[:, 256:320]).all()) and torch.equal(got[:, :256], x[:, :256]) and torch.equal(got[:, 320:], x[:, 320:])
+
+
+def _split_layers(n, k):
+    """Layers by which gate's product is a token's input 0 and up's its input 32."""
+    codes = B.slim_group_q4_tile(torch.full((n, k), 9, dtype=torch.uint8, device=DEV))
+    scales = torch.zeros(2, n, (k + 31) // 32, dtype=F16, device=DEV)
+    scales[0, :, 0] = scales[1, :, 1] = 1
+    return [B.SlimGroupQ4Weight(n, k, 32, codes, s.clone()) for s in scales]
+
+
+def _check_far(got, ref, rel):
+    """Relative bound `rel`, and one rounding to bf16, whose smallest numbers are 2^-133 apart (2^-139: what is lost where a factor itself falls below 2^-126)."""
+    got, low = _np(got), 2.0 ** -134 + 2.0 ** -139
+    there = np.abs(ref) < 3e38
+    assert np.isfinite(got[there]).all()
+    err = np.abs(got - ref)[there] - (np.abs(ref) * (rel + HALF[BF16] * (1 + rel)) + low)[there]
+    assert err.max() <= 0, err.max()
+
+
+@pytest.mark.parametrize("m,k", [(40, 64), (300, 64), (300, 8192)])
+def test_silu_far_out(m, k):
+    """silu(g) u where exp(g) is far below what binary32 holds and u makes up for it."""
+    n = 16
+    gate, up = _split_layers(n, k)
+    rng = np.random.default_rng(m)
+    X = torch.zeros(m, k, dtype=BF16, device=DEV)
+    X[:, 0] = torch.from_numpy(rng.uniform(-200, 20, m))
+    X[:, 32] = torch.from_numpy(2.0 ** rng.uniform(-20, 127.9, m) * rng.choice([-1, 1], m))
+    X[0, 0], X[0, 32], X[1, 0], X[1, 32], X[2, 0], X[2, 32] = -90.0, -90.0, -89.0, 1e30, -180.0, 3.3e38
+    H, G, U = B.slim_group_q4_gated(gate, up, X, G=True, U=True)
+    g, u = _np(X[:, :1]).repeat(n, 1), _np(X[:, 32:33]).repeat(n, 1)
+    assert (_np(G) == g).all() and (_np(U) == u).all()
+    _check_far(H, O.gated(g, u), (2 * np.abs(g) + 16) * U24)
+    assert float(H[0, 0]) != 0 and float(H[1, 0]) != 0 and float(H[2, 0]) != 0
+
+
+def test_gradients_of_silu_far_out():
+    m, n = 40, 128
+    rng = np.random.default_rng(0)
+    one, _ = _weights(n, 64, 32, False, 1)
+    new = lambda v: torch.from_numpy(v).to(BF16).to(DEV)
+    G, U, dH = new(rng.uniform(-200, 30, (m, n))), new(2.0 ** rng.uniform(-10, 100, (m, n)) * rng.choice([-1, 1], (m, n))), new(2.0 ** rng.uniform(-10, 20, (m, n)))
+    _, dG, dU = B.slim_group_q4_gated_backward(one, one, dH, G, U)
+    h, g, u = _np(dH), _np(G), _np(U)
+    s = O.sigma(g)
+    rg, ru = O.gated_backward(h, g, u)
+    rel = (2 * np.abs(g) + 16) * U24
+    _check_far(dU, ru, rel)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        _check_far(dG, rg, np.abs(h * u) * s * (1 + np.abs(g)) * rel / np.abs(rg))      # (the sum in it has terms of both signs)
