@@ -666,6 +666,7 @@ int slim_group_q4_gemm_t(const slim_group_q4_layer *layer, const void *dY, int64
  * slim_group_q4_gated_backward -- gradients through the block, its weights frozen:
  *   dU = dH silu(G),  dG = dH U sigma(G) (1 + G (1 - sigma(G))),  dX = dG Wg + dU Wu,
  * all of `dtype`; dG and dU [m][n] (what a low-rank term beside the layers needs) are rounded once, and dX is the product of the rounded ones.
+ * A G that is infinite (kept of a product that `dtype` does not hold) has the limits: dG = dU = 0 at -inf, dG = dH U and an infinite dU at inf.
  * dG may be G or dH, dU may be U or dH (same pointer and stride), not both the same; no other overlap.
  * Errors: NULL, SHAPE (the two layers' sizes too), ALIGN, WORKSPACE, HIP.
  */

@@ -220,9 +220,12 @@ __global__ __launch_bounds__(256) void gq4_act_backward_kernel(Gq4ActArgs a)
         load_piece<T, 8>(static_cast<const E *>(a.U) + row * a.u_ld, at, a.n, u);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
+            // (a G that overflowed when it was kept has the limits: at -inf both gradients are 0, at inf silu's is 1)
+            constexpr float kMost = 3.402823466e38f;
             const Gq4Sigma sigma(g[e]);
-            u[e] = (sigma.s * (1.f + g[e] * (1.f - sigma.s * sigma.h)) * h[e]) * (sigma.h * u[e]);
-            h[e] = (g[e] * sigma.s) * (sigma.h * h[e]);
+            const float low = fmaxf(g[e], -kMost);
+            u[e] = (sigma.s * (1.f + fminf(low, kMost) * (1.f - sigma.s * sigma.h)) * h[e]) * (sigma.h * u[e]);
+            h[e] = (low * sigma.s) * (sigma.h * h[e]);
         }
         store_piece<T, 8>(static_cast<E *>(a.dG) + row * a.dg_ld, at, a.n, u);
         store_piece<T, 8>(static_cast<E *>(a.dU) + row * a.du_ld, at, a.n, h);

@@ -159,3 +159,38 @@ def test_gradients_of_silu_far_out():
     _check_far(dU, ru, rel)
     with np.errstate(divide="ignore", invalid="ignore"):
         _check_far(dG, rg, np.abs(h * u) * s * (1 + np.abs(g)) * rel / np.abs(rg))      # (the sum in it has terms of both signs)
+
+
+def test_gradients_where_the_kept_product_overflowed():
+    """A product of -131000 is kept as -inf in fp16: silu and its gradient are 0 there, and so are dG and dU; of +131000, dG is dH U and dU is infinite."""
+    n, k, m = 64, 64, 70
+    gate, up = _split_layers(n, k)
+    gate.scales *= 2
+    X = _matrix(m, k, F16, 1)
+    X[1, 0], X[5, 0], X[7, 0] = -65504, -65504, 65504
+    H, G, U = B.slim_group_q4_gated(gate, up, X, G=True, U=True)
+    assert bool((H[1] == 0).all()) and bool(torch.isneginf(G[[1, 5]]).all()) and bool(torch.isposinf(G[7]).all())
+    dH = _matrix(m, n, F16, 2)
+    dX, dG, dU = B.slim_group_q4_gated_backward(gate, up, dH, G, U)
+    assert bool((dG[[1, 5]] == 0).all()) and bool((dU[[1, 5]] == 0).all()) and bool((dX[[1, 5]] == 0).all())
+    assert torch.equal(dG[7], (dH[7].float() * U[7].float()).half()) and torch.equal(dU[7], dH[7] * float("inf"))
+    rows = torch.arange(m, device=DEV) != 7
+    Vg, Vu = (_np(B.slim_group_q4_values(w, torch.float32)) for w in (gate, up))
+    rows[1] = rows[5] = False
+    _check_backward(dX[rows], dG[rows], dU[rows], dH[rows], G[rows], U[rows], Vg, Vu, F16)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_gradients_of_a_g_that_is_not_finite(dtype):
+    """NaN stays, in its own column and its token's dX."""
+    m, n = 3, 70
+    one, _ = _weights(n, 64, 32, False, 1)
+    G, U, dH = (_matrix(m, n, dtype, i) for i in range(3))
+    clean = [t.clone() for t in B.slim_group_q4_gated_backward(one, one, dH, G, U)]
+    G[1, 5], G[1, 6] = float("nan"), -float("inf")
+    dX, dG, dU = B.slim_group_q4_gated_backward(one, one, dH, G, U)
+    assert bool(torch.isnan(dX[1]).all()) and torch.equal(dX[::2], clean[0][::2])
+    for t, c in ((dG, clean[1]), (dU, clean[2])):
+        assert bool(torch.isnan(t[1, 5])) and float(t[1, 6]) == 0
+        t[1, 5:7] = c[1, 5:7]
+        assert torch.equal(t, c)
