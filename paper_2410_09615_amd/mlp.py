@@ -85,10 +85,10 @@ class GroupMlp:
         return slim.slim_group_q4_gemm(self.down, saved[0], Y=out, workspace=self._ws), saved if keep else None
 
     def backward(self, d_out: torch.Tensor, saved):
-        """The gradient of forward's output -> those of X, H, and (in the place of what was kept) G and U."""
+        """The gradient of forward's output -> those of X, H, G and U; what was kept is as it was."""
         _, G, U = saved
         dH = slim.slim_group_q4_gemm_t(self.down, d_out, workspace=self._ws)
-        dX, dG, dU = slim.slim_group_q4_gated_backward(self.gate, self.up, dH, G, U, dG=G, dU=U, workspace=self._ws)
+        dX, dG, dU = slim.slim_group_q4_gated_backward(self.gate, self.up, dH, G, U, workspace=self._ws)
         return dX, dH, dG, dU
 
 
