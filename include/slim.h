@@ -610,7 +610,8 @@ typedef struct {
     const uint8_t *zeros;   /* NULL: symmetric */
 } slim_group_q4_layer;
 
-/* Sizes in bytes (HOST out-pointers, NULL individually).  Errors: SHAPE (n, k < 1, k > 2^22, group not 32, 64 or 128). */
+/* Sizes in bytes (HOST out-pointers, NULL individually).  Errors: SHAPE (n, k < 1, k > 2^22, more than 2^26 - 4 blocks, 64 GiB
+ * of codes: what a launch has threads for; group not 32, 64 or 128). */
 int slim_group_q4_sizes(int32_t n, int32_t k, int32_t group, size_t *codes_bytes, size_t *scales_bytes, size_t *zeros_bytes);
 
 /*
@@ -668,7 +669,7 @@ int slim_group_q4_gemm_t(const slim_group_q4_layer *layer, const void *dY, int64
  * all of `dtype`; dG and dU [m][n] (what a low-rank term beside the layers needs) are rounded once, and dX is the product of the rounded ones.
  * A G that is infinite (kept of a product that `dtype` does not hold) has the limits: dG = dU = 0 at -inf, dG = dH U and an infinite dU at inf.
  * dG may be G or dH, dU may be U or dH (same pointer and stride), not both the same; no other overlap.
- * Errors: NULL, SHAPE (the two layers' sizes too), ALIGN, WORKSPACE, HIP.
+ * Errors: NULL, SHAPE (the two layers' sizes too; slim_group_q4_gated: n > 2^29 - 16), ALIGN, WORKSPACE, HIP.
  */
 int slim_group_q4_gated(const slim_group_q4_layer *gate, const slim_group_q4_layer *up, const void *X, int64_t x_ld, int32_t m, void *H, int64_t h_ld, void *G,
                         int64_t g_ld, void *U, int64_t u_ld, int32_t dtype, void *workspace, size_t workspace_bytes, void *stream);

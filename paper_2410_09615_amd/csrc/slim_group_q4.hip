@@ -332,9 +332,10 @@ using namespace slim;
 extern "C" int slim_group_q4_sizes(int32_t n, int32_t k, int32_t group, size_t *codes_bytes, size_t *scales_bytes, size_t *zeros_bytes)
 {
     const int shift = gq4_shift(group);
+    // (a launch has fewer than 2^32 threads: 64 to each block of codes where they are made or read back)
     if (n < 1 || k < 1 || k > kMaxK || n > (1 << 30) || shift < 0) return SLIM_ERR_SHAPE;
     const int64_t blocks = (int64_t)gq4_row_blocks(n) * gq4_col_blocks(k);
-    if (blocks > INT32_MAX) return SLIM_ERR_SHAPE;
+    if (blocks > (1 << 26) - 4) return SLIM_ERR_SHAPE;
     if (codes_bytes) *codes_bytes = (size_t)blocks * kGq4Block;
     if (scales_bytes) *scales_bytes = (size_t)n * gq4_groups(k, shift) * sizeof(half_t);
     if (zeros_bytes) *zeros_bytes = (size_t)n * gq4_groups(k, shift);

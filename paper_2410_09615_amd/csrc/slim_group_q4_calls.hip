@@ -150,7 +150,8 @@ extern "C" int slim_group_q4_gated(const slim_group_q4_layer *gate, const slim_g
     int shift;
     const int status = gq4_check_pair(gate, up, &shift);
     if (status == SLIM_ERR_NULL || status == SLIM_ERR_SHAPE) return status;
-    if (m < 1 || !half_dtype(dtype) || x_ld < gate->k || h_ld < gate->n || (G && g_ld < gate->n) || (U && u_ld < gate->n)) return SLIM_ERR_SHAPE;
+    // (a launch has fewer than 2^32 threads: where the weights of so many rows are streamed, 128 to each block of rows)
+    if (gate->n > (1 << 29) - kGq4Rows || m < 1 || !half_dtype(dtype) || x_ld < gate->k || h_ld < gate->n || (G && g_ld < gate->n) || (U && u_ld < gate->n)) return SLIM_ERR_SHAPE;
     if (status != SLIM_OK || !whole_elements(X, dtype) || !whole_elements(H, dtype) || !whole_elements(G, dtype) || !whole_elements(U, dtype)) return SLIM_ERR_ALIGN;
     const int room = gq4_check_room(gate->n, gate->k, m, SLIM_GROUP_Q4_GATED, workspace, workspace_bytes);
     if (room != SLIM_OK) return room;

@@ -185,3 +185,16 @@ def test_sizes_beyond_32_bits_are_refused():
                 lambda: B.SlimGroupQ4Weight(big, 64, 128, torch.zeros(4096, dtype=torch.uint8), torch.zeros(5, 1, dtype=torch.float16)).c_ref()):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_layers_that_no_launch_has_threads_for_are_refused():
+    """Fewer than 2^32 threads: 64 to a block of codes, and 128 to a block of rows of a gated pair."""
+    f = B.lib().slim_group_q4_sizes
+    rows = ((1 << 26) - 4) // 4 * 16                                  # of 512 inputs: 2^26 - 4 blocks
+    assert f(rows, 512, 128, None, None, None) == 0 and f(1 << 29, 128, 32, None, None, None) == 0 and f(16, 1 << 22, 128, None, None, None) == 0
+    for bad in ((1 << 30, 1), (rows + 1, 512), (1 << 21, 1 << 16)):
+        assert f(*bad, 128, None, None, None) == B.SLIM_ERR_SHAPE, bad
+        with pytest.raises(B.SlimError):
+            B.slim_group_q4_plan(*bad, 1)
+    big = _layer(n=(1 << 29) - 15, k=1)
+    assert B.lib().slim_group_q4_gated(big, big, A, 1, 1, A, 1 << 29, None, 0, None, 0, 0, None, 0, None) == B.SLIM_ERR_SHAPE
