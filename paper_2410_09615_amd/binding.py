@@ -853,6 +853,9 @@ class SlimGroupQ4Weight:
             _dev(self.scales, torch.float16, "scales")
             if self.codes.numel() != size["codes"] or self.scales.numel() * 2 != size["scales"] or self.scales.device != self.codes.device:
                 raise ValueError("codes and scales are not an n x k layer's on one device")
+            for name, t in (("scales", self.scales), ("zeros", self.zeros)):
+                if t is not None and t.dim() > 1 and t.shape[0] != self.n:
+                    raise ValueError(f"{name} must be [n][groups], row-major: transpose what a checkpoint holds as [groups][n]")
             if self.zeros is not None:
                 _dev(self.zeros, torch.uint8, "zeros")
                 if self.zeros.numel() != size["zeros"] or self.zeros.device != self.codes.device:

@@ -198,3 +198,15 @@ def test_layers_that_no_launch_has_threads_for_are_refused():
             B.slim_group_q4_plan(*bad, 1)
     big = _layer(n=(1 << 29) - 15, k=1)
     assert B.lib().slim_group_q4_gated(big, big, A, 1, 1, A, 1 << 29, None, 0, None, 0, 0, None, 0, None) == B.SLIM_ERR_SHAPE
+
+
+def test_scales_that_are_not_by_rows_are_refused(monkeypatch):
+    """[groups][n], as some checkpoints hold them, has a layer's number of elements too."""
+    monkeypatch.setattr(B, "_dev", lambda *a, **kw: None)             # (CPU tensors here; nothing is launched)
+    make = lambda scales, zeros=None: B.SlimGroupQ4Weight(64, 256, 128, torch.zeros(8192, dtype=torch.uint8), scales, zeros).c_ref()
+    s, z = torch.zeros(64, 2, dtype=torch.float16), torch.zeros(64, 2, dtype=torch.uint8)
+    for good in ((s, None), (s, z), (s.flatten(), z.flatten()), (s[:, :, None], None)):
+        make(*good)
+    for bad in ((s.t().contiguous(), None), (s, z.t().contiguous())):
+        with pytest.raises(ValueError, match="row-major"):
+            make(*bad)
