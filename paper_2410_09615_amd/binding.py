@@ -1000,7 +1000,9 @@ def _q4_product(name: str, transposed: bool, layer: SlimGroupQ4Weight, X: torch.
 
 def slim_group_q4_gemm(layer: SlimGroupQ4Weight, X: torch.Tensor, Y=None, workspace=None) -> torch.Tensor:
     """Y [m][n] = X W^T; X fp16 or bf16 [m][k], Y of its type (None: a new one), any row strides, any m >= 1.
-    workspace: alloc_group_q4_workspace's, or None for one of the call's own where it needs any."""
+    workspace: alloc_group_q4_workspace's, or None for one of the call's own where it needs any.
+    Autograd records nothing of this call or of slim_group_q4_gated, whatever X requires: their gradients are the calls slim_group_q4_gemm_t and
+    slim_group_q4_gated_backward, for a torch.autograd.Function's backward or a loop of one's own."""
     return _q4_product("slim_group_q4_gemm", False, layer, X, Y, workspace)
 
 
@@ -1016,7 +1018,8 @@ def _q4_pair(gate: SlimGroupQ4Weight, g: _LayerRef, up: SlimGroupQ4Weight, u: _L
 
 def slim_group_q4_gated(gate: SlimGroupQ4Weight, up: SlimGroupQ4Weight, X: torch.Tensor, H=None, G=None, U=None, workspace=None):
     """H [m][n] = silu(X Wg^T) * (X Wu^T) -> (H, G, U).  G, U: True for a new matrix that receives the two products (what
-    slim_group_q4_gated_backward wants), or one to write; None (returned as such): not wanted.  All of X's type, any row strides, any m >= 1."""
+    slim_group_q4_gated_backward wants), or one to write; None (returned as such): not wanted.  All of X's type, any row strides, any m >= 1.
+    No graph is recorded (slim_group_q4_gemm)."""
     ref, other = gate.c_ref(), up.c_ref()
     if H is None or G is True or U is True:
         new = lambda: torch.empty(X.shape[0], gate.n, dtype=X.dtype, device=gate.codes.device)
