@@ -651,7 +651,8 @@ int slim_group_q4_plan(int32_t n, int32_t k, int32_t m, int32_t call, int32_t *o
  * Sums in binary32, one rounding of each result.  Up to 48 tokens forward (on small layers up to 192: slim_group_q4_plan) weights are multiplied as whole numbers c - z and scales applied
  * to the sums; elsewhere a weight is (c - z) s rounded to `dtype` first, at most half a step of it: 1.9e-4 (fp16) or 1.5e-3 (bf16) of a result in the 2-norm beside the 2.1e-4 or
  * 1.7e-3 of its own rounding.  A token's result can so differ between calls of few and of many tokens.
- * Weights beyond fp16 (a scale of 256 or more, a large zero point) are no exception, but cost a second turn over the tile's weights; an infinite input of theirs makes the result NaN or infinite.
+ * Weights beyond fp16 (a scale of 256 or more, a large zero point) are no exception, but cost such a tile a turn of its own, four to seven
+ * times the call's time; an infinite input of theirs makes the result NaN or infinite.
  * X, Y (dY, dX) do not overlap.  Errors: NULL, SHAPE, ALIGN, WORKSPACE, HIP.
  */
 int slim_group_q4_gemm(const slim_group_q4_layer *layer, const void *X, int64_t x_ld, int32_t m, void *Y, int64_t y_ld, int32_t dtype, void *workspace,

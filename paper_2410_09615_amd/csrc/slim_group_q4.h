@@ -86,7 +86,8 @@ __device__ __forceinline__ half2_t gq4_less_zeros(uint32_t d, const Gq4Masks &k,
 // ---- scales that fp16 weights cannot have ----
 // (c - z) s reaches 255 x 65504, fp16 ends at 65504.  Where weights are rounded to fp16, groups whose scale is 256 or more are left out (a scale of 0; below that values stay below 256 x 255 =
 // 65280), and where a workgroup has met one it goes over its share once more for those alone, with weights and inputs as sums of two bf16 numbers (16 bits of a weight, all 11 of an input), whose
-// four products are added to the same sums.  Scales that are not finite stay with the others.  What it costs where there are none: six instructions for four scales, and a barrier.
+// four products are added to the same sums.  Scales that are not finite stay with the others.  What it costs where there are none: six instructions for four scales, and a barrier
+// (77 tokens' gradients through 5003 x 4100 24.5 -> 25.0 us, others within 1 %); where each row has one: 128 tokens on 4096 x 4096 20 -> 110 us, 4096 tokens 132 -> 813, their gradients 137 -> 1022.
 __device__ __forceinline__ bool gq4_large(uint32_t h) { return (h & 0x7fffu) - 0x5c00u < 0x2000u; }             // 256 to 65504, as bits of fp16
 // the scale if it is one of these (rest) or if it is none, and 0 otherwise
 __device__ __forceinline__ uint32_t gq4_scale_of(uint32_t h, bool rest) { return gq4_large(h) == rest ? h : 0u; }

@@ -6,7 +6,7 @@
 //   value = (c - z) s
 // Quotients in binary32.  All of these are bound by memory: quantization 4096 x 4096 fp16 13.1 us (3.2 TB/s; its 42 MB come from the last-level cache, all wavefronts
 // are there at once, and the life of one is a load, a reduction, codes and a store: instructions count, 17.7 us with a conversion, shift and two clamps per code and three for what is not finite), 10007 x 5003 fp32 with zero points in groups of 32 80 us (2.8 TB/s, rows at odd multiples of 4 bytes); values 10.0 and 56 us (4.2 TB/s); the activation's gradient,
-// 4096 x 11008 bf16, 73 us (6.2 TB/s).  The scale is rounded to fp16 before the codes are made, so codes are the nearest ones to the scale that is kept.
+// 4096 x 11008 bf16, 73 to 78 us (5.8 to 6.2 TB/s).  The scale is rounded to fp16 before the codes are made, so codes are the nearest ones to the scale that is kept.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

@@ -1,7 +1,8 @@
 // Gradients through frozen 4-bit weights that have a scale for each group of inputs:  dX = sum of dY_i W_i over one layer or the two of a gated block.
 // What is summed over are a layer's rows, so a lane's codes, which are inputs of one row, have to change places: a thread takes the same eight inputs of four rows, and a byte permutation
 // of two rows' dwords leaves pairs (row, row + 1) of one input side by side.  Codes become numbers of the gradients' type, (c - z) s rounded once to it, on their way into LDS.  Products
-// are summed in binary32 by the 32 x 32 x 16 matrix instructions, the weights as their A operand, and each result is rounded once.
+// are summed in binary32 by the 32 x 32 x 16 matrix instructions, the weights as their A operand, and each result is rounded once.  In fp16 groups whose scale makes weights beyond 65504 are left
+// to a turn of their own (gq4_large).
 #include <hip/hip_runtime.h>
 
 #include "slim_group_q4.h"
@@ -30,7 +31,7 @@ struct Gq4BackLds {
 // A workgroup has a tile of BT tokens x BO inputs and goes over the layers' rows 64 at a time.  KG groups of WR x WT wavefronts take turns at those pieces, each with two buffers of its own
 // in LDS.  While a piece is multiplied from one, the next one goes from registers into the other, and the one P further is asked for from memory into the registers that this frees: beside
 // each quarter of a piece's products (16 rows) stands a part of that work.  Rows that do not fill a piece are left for last and taken without that overlap.
-// Many tokens (256 x 256): 4096 through 8192 x 8192 in fp16 500 us, 1.10 PFLOP/s; through 2 x 11008 x 4096 in bf16 732 to 763 us with the activation's gradient (74), matrix pipes 58 % busy at 1.74 GHz.  LDS
+// Many tokens (256 x 256): 4096 through 8192 x 8192 in fp16 500 to 522 us from card to card, 1.05 to 1.10 PFLOP/s; through 2 x 11008 x 4096 in bf16 732 to 763 us with the activation's gradient (73 to 78), matrix pipes 58 % busy at 1.74 GHz.  LDS
 // carries 256 KiB for a piece's 256 products, about as long as they take, and the two overlap in part: without products 336 us of the 500, without stores to LDS 290.  (Half of the wavefronts at
 // products while the others store, in turn: 599 us.)  Smaller tiles are bound by the chain between two barriers, read, convert, store: 1.3 us a turn on 128 x 128 whose products take 0.2.
 template <class T, int SHIFT, int KG, int P, int WR, int WT, int AF, int BF>

@@ -2,14 +2,15 @@
 //   plain  Y = X W^T,     gated  H = silu(X Wg^T) * (X Wu^T), and where asked for G = X Wg^T and U = X Wu^T
 // A workgroup has a tile of BT tokens x BO rows of weights.  The tokens go through LDS; the weights do not: a wavefront has its own 64 rows, and a lane's 16 bytes of a
 // block of the layout are its operand of four 32 x 32 x 16 products once codes are numbers of the inputs' type, (c - z) s rounded once to it: the matrix instructions take 16 bits, and a scale
-// has 11 of them.  (Scales on the sums, as for few tokens, would take a second set of accumulators and, in groups of 32, as many additions as the products take cycles.)  LDS carries 160 KiB for
-// the 256 products of 64 inputs on 256 x 256, where it is 256 KiB if weights go there too, and each takes its turn then (4096 tokens on 8192 x 8192: 504 us, 491 so).
-// Products are summed in binary32, each result is rounded once.
-// Bound by power where there are many tokens: 4096 on 2 x 28672 x 8192 gated 3.30 to 3.55 ms from card to card, 1.08 to 1.17 PFLOP/s, matrix pipes 72 % busy of 5.1 M cycles at 1.5 GHz (the library's product of two fp16
+// has 11 of them.  (Scales on the sums, as for few tokens, would take a second set of accumulators and, in groups of 32, as many additions as the products take cycles.)  With
+// weights through LDS too it carries 256 KiB for a product's 256 x 256 x 64 instead of 160, and they take turns (a tile of 256 x 256, since replaced by two of 256 x 128 per compute unit: 4096 tokens on
+// 8192 x 8192 504 us with, 491 without).
+// Products are summed in binary32, each result is rounded once.  In fp16 groups whose scale makes weights beyond 65504 are left to a turn of their own (gq4_large).
+// Bound by power where there are many tokens: 4096 on 2 x 28672 x 8192 gated 3.30 to 3.55 ms from card to card, 1.08 to 1.17 PFLOP/s, matrix pipes 68 to 72 % busy at 1.5 GHz (the library's product of two fp16
 // matrices of 8192 x 8192: 1.34 PFLOP/s).  With few tiles by what a wavefront issues and waits for between two barriers: a step of 64 inputs takes 0.85 us on 256 x 128 with one workgroup per
-// compute unit, 0.5 on 256 x 64, 0.3 on 128 x 64 (the times at kRowShapes), where its products alone would take 0.43, 0.21 and 0.11; 333 tokens on 10007 x 4100 in groups of 32 52 us.
-// What is put between the products is placed by hand (a product, then vector instructions for its time): left to the compiler products stand in rows and the rest waits for them, 98 against
-// 79 us for 128 tokens on 4096 x 4096 in tiles of 256 x 256.  256 x 256 by eight wavefronts, weights converted twice: as fast as 256 x 128 with two workgroups per compute unit, and left out.
+// compute unit, 0.5 on 256 x 64, 0.3 on 128 x 64 (the times at kRowShapes), where its products alone would take 0.43, 0.21 and 0.11; 333 tokens on 10007 x 4100 in groups of 32 53 to 55 us.
+// What is put between the products is placed by hand (a product, then vector instructions for its time): on 256 x 128 left to the compiler 4096 tokens on 8192 x 8192 take 556 us, 502 so, 1024 on
+// 11008 x 4096 115 and 106 (the smaller tiles are as fast either way).
 #include <hip/hip_runtime.h>
 
 #include "slim_group_q4.h"

@@ -5,7 +5,7 @@
 // products start from zero and are added to the binary32 sums with its scale, so that a result is rounded once and nothing before it is.
 // The wavefronts' sums meet in LDS and are added in order.
 // Bound by memory in fp16 where the layer is large: 28672 x 8192 at one token 24.0 us, 5.0 TB/s (a large copy 5.15), 2 x 28672 x 8192 gated 49, at 16 tokens 28.4.  In bf16 a pair of codes takes five instructions
-// instead of two and a half, at 16 tokens 34 to 36 us, vector instructions 60 % of the cycles.  With 48 tokens by what is issued and by the tokens' way through the L2, which every
+// instead of two and a half: one token 31 us, 16 tokens 34 to 36, vector instructions 60 % of the cycles.  With 48 tokens by what is issued and by the tokens' way through the L2, which every
 // workgroup takes (13824 x 5120 gated, bf16, groups of 64: 424 MB of tokens to 77 of weights, 39 us).  4096 x 4096 at one token: the call's host time, 5 us (kernel 5).
 #include <hip/hip_runtime.h>
 
