@@ -194,3 +194,23 @@ def test_gradients_of_a_g_that_is_not_finite(dtype):
         assert bool(torch.isnan(t[1, 5])) and float(t[1, 6]) == 0
         t[1, 5:7] = c[1, 5:7]
         assert torch.equal(t, c)
+
+
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("m,n,k", [(3000, 200, 2600), (130, 4099, 8200), (70, 5003, 8200)])
+def test_weights_beyond_fp16_on_large_tiles(m, n, k, group):
+    """The same on tiles of 256 x 64, 256 x 128 and 256 x 256, alone and shared."""
+    (one, Va), (two, Vb) = _wide(n, k, group, 1, 2000), _wide(n, k, group, 2, 2000)
+    X, dY = _matrix(m, k, F16, 3, 2.0 ** -19), _matrix(m, n, F16, 4, 2.0 ** -16)
+    x, y = _np(X), _np(dY)
+    ref, mag = O.gemm(x, Va)
+    bound = _sum_bound(mag, k, x, F16)
+    _check(B.slim_group_q4_gemm(one, X), ref, bound, F16)
+    _, G, U = B.slim_group_q4_gated(one, two, X, G=True, U=True)
+    _check(G, ref, bound, F16)
+    ref, mag = O.gemm(x, Vb)
+    _check(U, ref, _sum_bound(mag, k, x, F16), F16)
+    ref, mag = O.gemm(y, Va.T)
+    _check(B.slim_group_q4_gemm_t(one, dY), ref, _sum_bound(mag, n, y, F16), F16)
+    G, U = _matrix(m, n, F16, 5), _matrix(m, n, F16, 6)
+    _check_backward(*B.slim_group_q4_gated_backward(one, two, dY, G, U), dY, G, U, Va, Vb, F16)
