@@ -610,8 +610,7 @@ typedef struct {
     const uint8_t *zeros;   /* NULL: symmetric */
 } slim_group_q4_layer;
 
-/* Sizes in bytes (HOST out-pointers, NULL individually).  Errors: SHAPE (n, k < 1, k > 2^22, more than 2^26 - 4 blocks, 64 GiB
- * of codes: what a launch has threads for; group not 32, 64 or 128). */
+/* Sizes in bytes (HOST out-pointers, NULL individually).  Errors: SHAPE (n, k < 1, n > 2^30, k > 2^22, group not 32, 64 or 128). */
 int slim_group_q4_sizes(int32_t n, int32_t k, int32_t group, size_t *codes_bytes, size_t *scales_bytes, size_t *zeros_bytes);
 
 /*
@@ -619,7 +618,7 @@ int slim_group_q4_sizes(int32_t n, int32_t k, int32_t group, size_t *codes_bytes
  * slim_group_q4_tile   -- row-major codes, a byte each (its low four bits; row stride ld bytes), to the blocks, for codes that a checkpoint brings;
  * slim_group_q4_untile is its inverse.
  * slim_group_q4_values -- what a layer's codes stand for, [n][k] rounded once to any slim_dtype.
- * Errors: NULL, SHAPE, ALIGN, HIP.
+ * Errors: NULL, SHAPE (slim_group_q4_weight, slim_group_q4_values: more than 2^26 - 4 blocks too, 64 GiB of codes, for which a launch has no threads), ALIGN, HIP.
  */
 int slim_group_q4_weight(const void *W, int64_t ld, int32_t dtype, int32_t n, int32_t k, int32_t group, uint8_t *codes, slim_half *scales, uint8_t *zeros,
                          void *stream);
@@ -653,7 +652,7 @@ int slim_group_q4_plan(int32_t n, int32_t k, int32_t m, int32_t call, int32_t *o
  * 1.7e-3 of its own rounding.  A token's result can so differ between calls of few and of many tokens.
  * Weights beyond fp16 (a scale of 256 or more, a large zero point) are no exception, but cost such a tile a turn of its own, four to seven
  * times the call's time; an infinite input of theirs makes the result NaN or infinite.
- * X, Y (dY, dX) do not overlap.  Errors: NULL, SHAPE, ALIGN, WORKSPACE, HIP.
+ * X, Y (dY, dX) do not overlap.  Errors: NULL, SHAPE (slim_group_q4_gemm: n > 2^30 - 32 too), ALIGN, WORKSPACE, HIP.
  */
 int slim_group_q4_gemm(const slim_group_q4_layer *layer, const void *X, int64_t x_ld, int32_t m, void *Y, int64_t y_ld, int32_t dtype, void *workspace,
                        size_t workspace_bytes, void *stream);
@@ -668,7 +667,7 @@ int slim_group_q4_gemm_t(const slim_group_q4_layer *layer, const void *dY, int64
  * slim_group_q4_gated_backward -- gradients through the block, its weights frozen:
  *   dU = dH silu(G),  dG = dH U sigma(G) (1 + G (1 - sigma(G))),  dX = dG Wg + dU Wu,
  * all of `dtype`; dG and dU [m][n] (what a low-rank term beside the layers needs) are rounded once, and dX is the product of the rounded ones.
- * A G that is infinite (kept of a product that `dtype` does not hold) has the limits: dG = dU = 0 at -inf, dG = dH U and an infinite dU at inf.
+ * A G that is infinite (kept of a product that `dtype` does not hold) has the limits: dG = dU = 0 at -inf, dG = dH U and dU = dH times infinity at inf.
  * dG may be G or dH, dU may be U or dH (same pointer and stride), not both the same; no other overlap.
  * Errors: NULL, SHAPE (the two layers' sizes too; slim_group_q4_gated: n > 2^29 - 16), ALIGN, WORKSPACE, HIP.
  */

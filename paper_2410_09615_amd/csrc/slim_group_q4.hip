@@ -332,21 +332,23 @@ using namespace slim;
 extern "C" int slim_group_q4_sizes(int32_t n, int32_t k, int32_t group, size_t *codes_bytes, size_t *scales_bytes, size_t *zeros_bytes)
 {
     const int shift = gq4_shift(group);
-    // (a launch has fewer than 2^32 threads: 64 to each block of codes where they are made or read back)
     if (n < 1 || k < 1 || k > kMaxK || n > (1 << 30) || shift < 0) return SLIM_ERR_SHAPE;
     const int64_t blocks = (int64_t)gq4_row_blocks(n) * gq4_col_blocks(k);
-    if (blocks > (1 << 26) - 4) return SLIM_ERR_SHAPE;
+    if (blocks > INT32_MAX) return SLIM_ERR_SHAPE;
     if (codes_bytes) *codes_bytes = (size_t)blocks * kGq4Block;
     if (scales_bytes) *scales_bytes = (size_t)n * gq4_groups(k, shift) * sizeof(half_t);
     if (zeros_bytes) *zeros_bytes = (size_t)n * gq4_groups(k, shift);
     return SLIM_OK;
 }
 
+// A launch has fewer than 2^32 threads: 64 to each block of codes where they are made or read back.
+static bool gq4_has_threads(int n, int k) { return (int64_t)gq4_row_blocks(n) * gq4_col_blocks(k) <= (1 << 26) - 4; }
+
 extern "C" int slim_group_q4_weight(const void *W, int64_t ld, int32_t dtype, int32_t n, int32_t k, int32_t group, uint8_t *codes, slim_half *scales,
                                     uint8_t *zeros, void *stream)
 {
     if (!W || !codes || !scales) return SLIM_ERR_NULL;
-    if (slim_group_q4_sizes(n, k, group, nullptr, nullptr, nullptr) != SLIM_OK || ld < k || (!half_dtype(dtype) && dtype != SLIM_F32)) return SLIM_ERR_SHAPE;
+    if (slim_group_q4_sizes(n, k, group, nullptr, nullptr, nullptr) != SLIM_OK || ld < k || (!half_dtype(dtype) && dtype != SLIM_F32) || !gq4_has_threads(n, k)) return SLIM_ERR_SHAPE;
     if (!whole_elements(W, dtype) || !aligned16(codes) || (reinterpret_cast<uintptr_t>(scales) & 1u)) return SLIM_ERR_ALIGN;
     const int shift = gq4_shift(group);
     const Gq4QuantArgs a{W, ld, n, k, gq4_col_blocks(k), gq4_groups(k, shift), (int64_t)gq4_row_blocks(n) * gq4_col_blocks(k), codes,
@@ -397,7 +399,7 @@ extern "C" int slim_group_q4_values(const slim_group_q4_layer *layer, void *out,
     int shift;
     const int status = gq4_check(layer, &shift);
     if (status != SLIM_OK) return status;
-    if (ld < layer->k || (!half_dtype(dtype) && dtype != SLIM_F32)) return SLIM_ERR_SHAPE;
+    if (ld < layer->k || (!half_dtype(dtype) && dtype != SLIM_F32) || !gq4_has_threads(layer->n, layer->k)) return SLIM_ERR_SHAPE;
     if (!whole_elements(out, dtype)) return SLIM_ERR_ALIGN;
     const Gq4Weights w = gq4_weights(layer);
     hipStream_t st = static_cast<hipStream_t>(stream);

@@ -21,6 +21,8 @@ int64_t gq4_back_workspace(int n, int k, int m, int terms);
 
 // The kernels address a tile's tokens by 32 bits from the first one on; with longer rows a call goes token by token.
 constexpr int64_t kLongRow = 1 << 23;
+// A launch has fewer than 2^32 threads: where the weights of so many rows are streamed 128 to each two blocks of rows, or to each of a gated pair.
+constexpr int kMostRows = (1 << 30) - 2 * kGq4Rows;
 
 // Both layers of a gated block: of one shape and group.
 static int gq4_check_pair(const slim_group_q4_layer *gate, const slim_group_q4_layer *up, int *shift)
@@ -120,7 +122,7 @@ extern "C" int slim_group_q4_gemm(const slim_group_q4_layer *layer, const void *
     int shift;
     const int status = gq4_check(layer, &shift);
     if (status == SLIM_ERR_NULL || status == SLIM_ERR_SHAPE) return status;
-    if (m < 1 || !half_dtype(dtype) || x_ld < layer->k || y_ld < layer->n) return SLIM_ERR_SHAPE;
+    if (layer->n > kMostRows || m < 1 || !half_dtype(dtype) || x_ld < layer->k || y_ld < layer->n) return SLIM_ERR_SHAPE;
     if (status != SLIM_OK || !whole_elements(X, dtype) || !whole_elements(Y, dtype)) return SLIM_ERR_ALIGN;
     const int room = gq4_check_room(layer->n, layer->k, m, SLIM_GROUP_Q4_GEMM, workspace, workspace_bytes);
     if (room != SLIM_OK) return room;
@@ -150,8 +152,7 @@ extern "C" int slim_group_q4_gated(const slim_group_q4_layer *gate, const slim_g
     int shift;
     const int status = gq4_check_pair(gate, up, &shift);
     if (status == SLIM_ERR_NULL || status == SLIM_ERR_SHAPE) return status;
-    // (a launch has fewer than 2^32 threads: where the weights of so many rows are streamed, 128 to each block of rows)
-    if (gate->n > (1 << 29) - kGq4Rows || m < 1 || !half_dtype(dtype) || x_ld < gate->k || h_ld < gate->n || (G && g_ld < gate->n) || (U && u_ld < gate->n)) return SLIM_ERR_SHAPE;
+    if (gate->n > kMostRows / 2 || m < 1 || !half_dtype(dtype) || x_ld < gate->k || h_ld < gate->n || (G && g_ld < gate->n) || (U && u_ld < gate->n)) return SLIM_ERR_SHAPE;
     if (status != SLIM_OK || !whole_elements(X, dtype) || !whole_elements(H, dtype) || !whole_elements(G, dtype) || !whole_elements(U, dtype)) return SLIM_ERR_ALIGN;
     const int room = gq4_check_room(gate->n, gate->k, m, SLIM_GROUP_Q4_GATED, workspace, workspace_bytes);
     if (room != SLIM_OK) return room;

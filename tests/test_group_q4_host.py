@@ -188,16 +188,19 @@ def test_sizes_beyond_32_bits_are_refused():
 
 
 def test_layers_that_no_launch_has_threads_for_are_refused():
-    """Fewer than 2^32 threads: 64 to a block of codes, and 128 to a block of rows of a gated pair."""
-    f = B.lib().slim_group_q4_sizes
+    """Fewer than 2^32 threads: 64 to a block of codes that is made or read back, 128 to two blocks of rows that are streamed, or to one of a gated pair.  (Nothing is launched: the first refusal
+    of what would have been is that of an odd address.)"""
+    L = B.lib()
     rows = ((1 << 26) - 4) // 4 * 16                                  # of 512 inputs: 2^26 - 4 blocks
-    assert f(rows, 512, 128, None, None, None) == 0 and f(1 << 29, 128, 32, None, None, None) == 0 and f(16, 1 << 22, 128, None, None, None) == 0
-    for bad in ((1 << 30, 1), (rows + 1, 512), (1 << 21, 1 << 16)):
-        assert f(*bad, 128, None, None, None) == B.SLIM_ERR_SHAPE, bad
-        with pytest.raises(B.SlimError):
-            B.slim_group_q4_plan(*bad, 1)
-    big = _layer(n=(1 << 29) - 15, k=1)
-    assert B.lib().slim_group_q4_gated(big, big, A, 1, 1, A, 1 << 29, None, 0, None, 0, 0, None, 0, None) == B.SLIM_ERR_SHAPE
+    weight = lambda n, k: L.slim_group_q4_weight(ODD, k, 0, n, k, 128, A, A, None, None)
+    values = lambda n, k: L.slim_group_q4_values(_layer(n=n, k=k), ODD, k, 0, None)
+    gemm = lambda n, k: L.slim_group_q4_gemm(_layer(n=n, k=k), ODD, k, 1, A, n, 0, None, 0, None)
+    gated = lambda n, k: L.slim_group_q4_gated(_layer(n=n, k=k), _layer(n=n, k=k), ODD, k, 1, A, n, None, 0, None, 0, 0, None, 0, None)
+    for f in (weight, values):
+        assert f(rows, 512) == f(1 << 29, 128) == f(16, 1 << 22) == B.SLIM_ERR_ALIGN
+        assert f(rows + 1, 512) == f(1 << 30, 1) == f(1 << 21, 1 << 16) == B.SLIM_ERR_SHAPE
+    assert gemm((1 << 30) - 32, 1) == gemm(1 << 21, 1 << 16) == gated((1 << 29) - 16, 1) == gated(1 << 21, 1 << 16) == B.SLIM_ERR_ALIGN
+    assert gemm((1 << 30) - 31, 1) == gated((1 << 29) - 15, 1) == B.SLIM_ERR_SHAPE
 
 
 def test_scales_that_are_not_by_rows_are_refused(monkeypatch):
